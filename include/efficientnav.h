@@ -20,6 +20,10 @@
  *                               new-group decision
  *   kv_pool_append              new objects' KV saved at the end of their group
  *   segmented_decode_step       one decode step over the context gathered once
+ *   segmented_tree_attention    a step over a tree of drafted tokens instead;
+ *   token_tree_accept,          which of them the model confirms, their keys and
+ *   segmented_tree_commit       values into the context, and what the next token
+ *   token_rules_apply           may be (penalties, biases, masks on logits)
  *   kv_tier_*                   which groups are in device memory, loads of the
  *                               others from a host store, cache hit rate
  *
@@ -364,6 +368,163 @@ int segmented_decode_step_static(en_pool *pool, en_plan *plan, int32_t q_first, 
                                  void *kc_dev, void *vt_dev, void *out_dev, float *mass_out_dev,
                                  void *stream);
 
+/* ------------------------------------------------------------------------
+ * Decoding with drafted tokens (Section 3.2: about 40 tokens are decoded over a
+ * context that was gathered once, and each step of one token reads all of it).
+ * A draft proposes a tree of tokens per agent, one step of the model looks at
+ * all of them, and the path that the model's own choices confirm joins the
+ * context:
+ *   per layer  segmented_tree_attention      (the context is only read)
+ *   once       token_tree_accept             (which nodes; the next token)
+ *   per step   segmented_tree_commit         (all layers in one launch)
+ * Everything that changes from step to step is device memory, so that a loop
+ * of steps needs no word from the host and can be captured into a HIP graph.
+ *
+ * Trees. n_nodes <= EN_TREE_MAX_NODES drafted tokens per agent, the same number
+ * for all, and
+ *   parent_dev : device int32 [B, n_nodes], the node whose child node i is: -1
+ *                (it follows the context's last token) or a node before it,
+ *                0 <= parent < i. With any other value node i is absent (the
+ *                padding of a smaller tree), and so are its descendants.
+ *   done_dev   : device int32 [B], the new tokens that agent's context holds
+ *                already, 0 .. N_q; with any other value (an idle agent) every
+ *                node of the agent is absent.
+ * Node i's way is the nodes from a root down to it, itself included; its depth
+ * is how many of them come before it. It sits at position L_c + done + depth; a
+ * node with done + depth >= N_q has no place in the plan's reserve and is
+ * absent.
+ */
+#define EN_TREE_MAX_NODES 64
+
+/* Attention of the tree's nodes over the L_c + done tokens of the context and
+ * the nodes of their own way (as rows of one prefill over each way by itself).
+ * Queries and the nodes' keys are rotated at the nodes' positions, here; the
+ * context buffers are not written, and rows from L_c + done on are not looked
+ * at. With a chain (parent_i = i - 1) the result is that of
+ * segmented_decode_step(q_first = done).
+ *   q_dev                  : device, [B, n_nodes, Hq, D], unrotated
+ *   k_rows_dev, v_rows_dev : device, [B, n_nodes, Hkv, D], keys unrotated
+ *   kc_dev, vt_dev         : the context buffers filled by gather_rope
+ *   out_dev                : device, [B, n_nodes, Hq, D]; rows of absent nodes
+ *                            are set to zero
+ *   ws_dev, ws_bytes       : scratch of at least en_tree_workspace_bytes, 16-byte
+ *                            aligned, or NULL where that is 0
+ * Arrays of rows and contexts are 16-byte aligned. What absent nodes' rows
+ * hold, or nodes outside a way, makes no difference, infinities and NaN
+ * included.
+ * Errors: INVALID_ARG (null, n_nodes < 1, alignment), UNSUPPORTED (n_nodes >
+ *         EN_TREE_MAX_NODES, a plan whose values stay in the pool, 2^31 rows or
+ *         contexts of 2^31 bytes per KV head), CAPACITY (ws_bytes), DEVICE.
+ */
+size_t en_tree_workspace_bytes(const en_pool *pool, const en_plan *plan, int32_t n_nodes);
+int segmented_tree_attention(en_pool *pool, en_plan *plan, int32_t n_nodes, const int32_t *done_dev,
+                             const int32_t *parent_dev, const void *q_dev, const void *k_rows_dev,
+                             const void *v_rows_dev, const void *kc_dev, const void *vt_dev, void *out_dev,
+                             void *ws_dev, size_t ws_bytes, void *stream);
+
+/* What a token's logit becomes before the next token is chosen. c is how often
+ * token v has occurred: in the first history_len[b] entries of the agent's
+ * history and among the tokens of the node's way. In float32, every operation
+ * rounded:
+ *   c > 0    : x = x > 0 ? x / repetition : x * repetition,
+ *              x = (x - c * frequency) - presence
+ *   bias     : x = x + bias[v]
+ *   mask     : x = -infinity where token v's bit is 0
+ * Every part may be left out (NULL).
+ *   penalties_dev   : device float [B, 3]: repetition, frequency, presence
+ *                     (1, 0, 0 changes nothing); read with the history
+ *   history_dev     : device int32 [B, history_stride]; entries that are no
+ *                     token (outside [0, vocab)) count nowhere. NULL: only ways
+ *   history_len_dev : device int32 [B]; taken as 0 below it and as
+ *                     history_stride beyond it
+ *   bias_dev        : device float, row b at b * bias_agent_stride (0: one row
+ *                     for all), [vocab] each
+ *   mask_dev        : device uint32, row (b, i) at b * mask_agent_stride + i *
+ *                     mask_node_stride (0: one row for all), (vocab + 31) / 32
+ *                     words each, bit v % 32 of word v / 32
+ */
+typedef struct en_token_rules {
+    const float *penalties_dev;
+    const int32_t *history_dev;
+    const int32_t *history_len_dev;
+    const float *bias_dev;
+    const uint32_t *mask_dev;
+    int64_t bias_agent_stride;
+    int64_t mask_agent_stride;
+    int64_t mask_node_stride;
+    int32_t history_stride;
+    int32_t reserved;         /* must be 0 */
+} en_token_rules;
+
+/* The rules applied to logits, for a caller that samples from them.
+ *   parent_dev, tokens_dev : device int32 [B, n_nodes], the tree and its nodes'
+ *                     tokens; both NULL: the rows stand by themselves (plain
+ *                     decoding: n_nodes = 1), their ways are empty
+ *   logits_dev      : device, row (b, i) at (b * n_nodes + i) * logits_stride,
+ *                     `vocab` values of dtype (EN_F32 or EN_BF16)
+ *   out_dev         : the same, with out_stride, rounded once; may be logits_dev
+ *                     (with the same stride), else the two must not overlap.
+ *                     Rows of absent nodes are left as they are. (A node is absent
+ *                     by parent_dev alone here.)
+ * Errors: INVALID_ARG (null, non-positive sizes, strides below vocab,
+ *         alignment to an element), UNSUPPORTED (dtype, n_nodes >
+ *         EN_TREE_MAX_NODES), DEVICE.
+ */
+int token_rules_apply(const en_token_rules *rules, int32_t n_agents, int32_t n_nodes, int32_t vocab, int32_t dtype,
+                      const int32_t *parent_dev, const int32_t *tokens_dev, const void *logits_dev,
+                      int64_t logits_stride, void *out_dev, int64_t out_stride, void *stream);
+
+/* Which drafted tokens the model confirms. choice_i is the token with the
+ * largest logit of node i under the rules (NULL: none), the lowest among equals;
+ * NaN never wins, and -1 where nothing is above -infinity. The path begins with
+ * node 0, the token that the last step left to be looked at (parent -1; without
+ * it, or where it is absent, the path is empty), and goes on with the lowest
+ * child of its last node whose token is that node's choice.
+ *   tokens_dev     : device int32 [B, n_nodes]
+ *   logits_dev     : as token_rules_apply, or NULL: choice_dev holds the choices
+ *                    (a caller that sampled them); vocab, dtype, rules unused
+ *   choice_dev     : device int32 [B, n_nodes]; written if there are logits (-1
+ *                    for absent nodes; may be NULL), else read
+ *   path_dev       : device int32 [B, n_nodes], the path's nodes, then -1
+ *   n_accepted_dev : device int32 [B], its length
+ *   next_dev       : device int32 [B], choice of the path's last node (the next
+ *                    step's node 0), -1 for an empty path
+ *   done_out_dev   : device int32 [B], done + n_accepted; may be done_dev
+ *   ws_dev         : scratch of at least en_tree_accept_workspace_bytes, 8-byte
+ *                    aligned; NULL without logits
+ * With n_nodes = 1 and parent -1 this is a greedy choice for plain decoding.
+ * Errors: as token_rules_apply, CAPACITY (ws_bytes).
+ */
+size_t en_tree_accept_workspace_bytes(const en_plan *plan, int32_t n_nodes, int32_t vocab);
+int token_tree_accept(const en_plan *plan, const en_token_rules *rules, int32_t n_nodes, int32_t vocab, int32_t dtype,
+                      const int32_t *done_dev, const int32_t *parent_dev, const int32_t *tokens_dev,
+                      const void *logits_dev, int64_t logits_stride, int32_t *choice_dev, int32_t *path_dev,
+                      int32_t *n_accepted_dev, int32_t *next_dev, int32_t *done_out_dev, void *ws_dev,
+                      size_t ws_bytes, void *stream);
+
+/* The accepted nodes' keys and values join the contexts of n_layers layers, in
+ * one launch per EN_TREE_COMMIT_LAYERS of them: entry j of the path goes to
+ * context row L_c + (done - n_accepted) + j, the key rotated there, as
+ * segmented_decode_step writes its rows.
+ *   done_dev                 : device int32 [B], the counts AFTER the acceptance
+ *                              (token_tree_accept's done_out_dev)
+ *   n_accepted_dev, path_dev : from token_tree_accept
+ *   k_rows_dev, v_rows_dev   : host arrays [n_layers] of device pointers, the rows
+ *                              that each layer's segmented_tree_attention got
+ *   kc_dev, vt_dev           : host arrays [n_layers] of device pointers, the
+ *                              layers' context buffers of this plan
+ * The arrays of pointers are read before the call returns. Entries that are no
+ * node, and rows outside the plan's reserve, are left out; no other row is
+ * written.
+ * Errors: INVALID_ARG (null, n_layers < 0, n_nodes < 1, alignment), UNSUPPORTED
+ *         (n_nodes > EN_TREE_MAX_NODES, a plan whose values stay in the pool),
+ *         DEVICE.
+ */
+#define EN_TREE_COMMIT_LAYERS 64
+int segmented_tree_commit(en_pool *pool, en_plan *plan, int32_t n_nodes, int32_t n_layers, const int32_t *done_dev,
+                          const int32_t *n_accepted_dev, const int32_t *path_dev, const void *const *k_rows_dev,
+                          const void *const *v_rows_dev, void *const *kc_dev, void *const *vt_dev, void *stream);
+
 /* Per-segment attention mass (Section 3.3: the attention between newly
  * detected objects and an existing group) from the scratch left by the
  * attention call on the same plan and stream.
@@ -520,9 +681,9 @@ int kv_tier_destroy(en_tier *tier);
  * Measurement aid for callers that need the duration of the attention kernel
  * itself (the kernel the roofline is quoted on), not of the whole call.
  * en_timing_enable(pool, n > 0) creates n pairs of HIP events in the pool; from
- * then on every segmented_prefill_attention / segmented_decode_step call on that
- * pool records one pair around its main kernel launch, on the stream it launches
- * on, until n pairs are used. en_timing_enable(pool, 0) frees them (so does
+ * then on every segmented_prefill_attention / segmented_decode_step /
+ * segmented_tree_attention call on that pool records one pair around its main
+ * kernel launch, on the stream it launches on, until n pairs are used. en_timing_enable(pool, 0) frees them (so does
  * kv_pool_destroy). en_timing_collect waits for the recorded pairs, writes their
  * durations in milliseconds to ms_out_host (at most cap) and resets the record
  * count. The state belongs to the pool: calls on one pool are serialised by the

@@ -34,7 +34,10 @@ EXPORTS = [
     "kv_tier_select_scored",
     "kv_tier_fetch", "kv_tier_fence", "kv_tier_prefetch", "kv_tier_get_stats", "kv_tier_residency",
     "kv_tier_destroy",
+    "en_tree_workspace_bytes", "segmented_tree_attention", "token_rules_apply", "en_tree_accept_workspace_bytes",
+    "token_tree_accept", "segmented_tree_commit",
 ]
+TREE_MAX_NODES = 64
 
 
 class EnError(RuntimeError):
@@ -58,6 +61,13 @@ class PlanInfo(C.Structure):
 class TierStats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("fetches", "requested", "hits", "prefetched", "misses", "loads",
                                          "bytes_loaded", "evictions")]
+
+
+class _TokenRules(C.Structure):
+    _fields_ = [("penalties_dev", C.c_void_p), ("history_dev", C.c_void_p), ("history_len_dev", C.c_void_p),
+                ("bias_dev", C.c_void_p), ("mask_dev", C.c_void_p), ("bias_agent_stride", C.c_int64),
+                ("mask_agent_stride", C.c_int64), ("mask_node_stride", C.c_int64), ("history_stride", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -124,9 +134,18 @@ def load(path: Optional[str] = None) -> C.CDLL:
     lib.kv_tier_get_stats.argtypes = [vp, C.POINTER(TierStats)]
     lib.kv_tier_residency.argtypes = [vp, i32p]
     lib.kv_tier_destroy.argtypes = [vp]
+    lib.en_tree_workspace_bytes.argtypes = [vp, vp, C.c_int32]
+    lib.en_tree_workspace_bytes.restype = C.c_size_t
+    lib.segmented_tree_attention.argtypes = [vp, vp, C.c_int32, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.token_rules_apply.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, C.c_int64, vp, C.c_int64, vp]
+    lib.en_tree_accept_workspace_bytes.argtypes = [vp, C.c_int32, C.c_int32]
+    lib.en_tree_accept_workspace_bytes.restype = C.c_size_t
+    lib.token_tree_accept.argtypes = [vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_int64, vp, vp, vp, vp, vp, vp,
+                                      C.c_size_t, vp]
+    lib.segmented_tree_commit.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("en_context_bytes", "en_workspace_bytes", "en_decode_workspace_bytes", "en_last_error",
-                        "kv_tier_slot_bytes", "kv_tier_pool"):
+                        "kv_tier_slot_bytes", "kv_tier_pool", "en_tree_workspace_bytes", "en_tree_accept_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -196,8 +215,8 @@ class Pool:
 
 
 class Plan:
-    def __init__(self, handle, pool: Pool):
-        self.handle, self.pool = handle, pool
+    def __init__(self, handle, pool: Pool, n_agents: int = 1):
+        self.handle, self.pool, self.n_agents = handle, pool, n_agents
         pool._plans.add(self)
 
     @property
@@ -290,7 +309,7 @@ def segment_select(pool: Pool, sel, sel_ptr, n_new: int) -> Plan:
     h = C.c_void_p()
     _check(load().segment_select(pool.handle, len(sel_ptr) - 1, _ip(sel), _ip(sel_ptr), n_new,
                                  C.byref(h)))
-    return Plan(h, pool)
+    return Plan(h, pool, len(sel_ptr) - 1)
 
 
 def segment_select_scored(pool: Pool, p, threshold: float, budget_tokens: int, n_new: int,
@@ -413,6 +432,187 @@ def segmented_decode_step_static(pool: Pool, plan: Plan, q_first: int, q, k_rows
         kc.data_ptr(), vt.data_ptr(), out.data_ptr(), mass_out.data_ptr() if mass_out is not None else None,
         _stream(stream)))
     return out
+
+
+def _shaped(name: str, t, shape, dtypes):
+    """A contiguous tensor of the current device, of that shape and one of these types; its address."""
+    if t.shape != shape or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}{'' if t.is_contiguous() else ', not contiguous'}; "
+                         f"a contiguous {tuple(shape)} of {' or '.join(str(x) for x in dtypes)} is wanted")
+    _on_current_device(name, t)
+    return t.data_ptr()
+
+
+_current_device = None
+
+
+def _on_current_device(name: str, t):
+    """Launches go to the current device: a tensor elsewhere would be read there by address."""
+    global _current_device
+    if not t.is_cuda:
+        raise ValueError(f"{name}: on {t.device}, not on a GPU")
+    if _current_device is None:
+        import torch
+        torch.cuda.current_device()          # sets the device up if nothing has yet
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if t.get_device() != _current_device():
+        raise ValueError(f"{name}: on {t.device}, not on the current device")
+
+
+def _torch_types(desc: PoolDesc):
+    import torch
+    return (torch.float32,) if desc.dtype == EN_F32 else (torch.bfloat16,)
+
+
+def tree_workspace_bytes(pool: Pool, plan: Plan, n_nodes: int) -> int:
+    return int(load().en_tree_workspace_bytes(pool.handle, plan.handle, int(n_nodes)))
+
+
+def _room(name: str, t, nbytes: int):
+    """Address and bytes of a buffer of at least `nbytes` on the current device."""
+    have = t.numel() * t.element_size()
+    if have < nbytes or not t.is_contiguous():
+        raise ValueError(f"{name}: {have} bytes, {nbytes} contiguous ones are wanted")
+    _on_current_device(name, t)
+    return t.data_ptr(), have
+
+
+def segmented_tree_attention(pool: Pool, plan: Plan, done, parent, q, k_rows, v_rows, kc, vt, out, ws=None, stream=None):
+    """done int32 [B], parent int32 [B, n]; q, out [B, n, Hq, D], k_rows/v_rows [B, n, Hkv, D] in the contexts' type."""
+    import torch
+    d, n, ints = pool.desc, int(q.shape[1]), (torch.int32,)
+    b, types, ctx = int(q.shape[0]), _torch_types(d), context_bytes(pool, plan)
+    if b != plan.n_agents:
+        raise ValueError(f"q: {b} agents, the plan has {plan.n_agents}")
+    rows, mine = (b, n, d.n_q_heads, d.head_dim), (b, n, d.n_kv_heads, d.head_dim)
+    wsp, wsb = _room("ws", ws, 0) if ws is not None else (None, 0)
+    _check(load().segmented_tree_attention(
+        pool.handle, plan.handle, n, _shaped("done", done, (b,), ints), _shaped("parent", parent, (b, n), ints),
+        _shaped("q", q, rows, types), _shaped("k_rows", k_rows, mine, types), _shaped("v_rows", v_rows, mine, types),
+        _room("kc", kc, ctx)[0], _room("vt", vt, ctx)[0], _shaped("out", out, rows, types), wsp, wsb, _stream(stream)))
+    return out
+
+
+class TokenRules:
+    """Rules on logits; keeps their tensors alive. See token_rules."""
+
+    def __init__(self, struct: _TokenRules, tensors: dict):
+        self.struct, self.tensors = struct, tensors
+        self.address = C.addressof(struct)
+
+    def check(self, n_agents: int, n_nodes: int, vocab: int):
+        t = self.tensors
+        words = (vocab + 31) // 32
+        for name, x in t.items():
+            if x is None:
+                continue
+            _on_current_device(name, x)
+            if x.shape[0] != n_agents and not (name == "bias" and x.dim() == 1):
+                raise ValueError(f"{name}: {tuple(x.shape)} for {n_agents} agents")
+        if t["bias"] is not None and t["bias"].shape[-1] < vocab:
+            raise ValueError(f"bias: {tuple(t['bias'].shape)} for {vocab} tokens")
+        if t["mask"] is not None and (t["mask"].shape[1] not in (1, n_nodes) or t["mask"].shape[2] < words):
+            raise ValueError(f"mask: {tuple(t['mask'].shape)} for {n_nodes} nodes and {words} words")
+
+
+def token_rules(penalties=None, history=None, history_len=None, bias=None, mask=None) -> TokenRules:
+    """penalties float32 [B, 3] (repetition, frequency, presence); history int32 [B, H] with history_len int32 [B]; bias
+    float32 [vocab] or [B, vocab]; mask int32 [B, 1 or n, words], bit v % 32 of word v / 32. Each may be None."""
+    import torch
+    want = {"penalties": (penalties, torch.float32, (2,)), "history": (history, torch.int32, (2,)),
+            "history_len": (history_len, torch.int32, (1,)), "bias": (bias, torch.float32, (1, 2)), "mask": (mask, torch.int32, (3,))}
+    for name, (x, dtype, dims) in want.items():
+        if x is not None and (x.dtype != dtype or x.dim() not in dims or not x.is_contiguous()):
+            raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype}; a contiguous {dtype} of {dims} axes is wanted")
+    if penalties is not None and penalties.shape[1] != 3:
+        raise ValueError(f"penalties: {tuple(penalties.shape)}, not [B, 3]")
+    if (history is None) != (history_len is None):
+        raise ValueError("history and history_len go together")
+    at = lambda x: None if x is None else x.data_ptr()
+    s = _TokenRules(at(penalties), at(history), at(history_len), at(bias), at(mask),
+                    bias.shape[1] if bias is not None and bias.dim() == 2 else 0,
+                    mask.shape[1] * mask.shape[2] if mask is not None else 0,
+                    mask.shape[2] if mask is not None and mask.shape[1] > 1 else 0,
+                    history.shape[1] if history is not None else 0, 0)
+    return TokenRules(s, {name: x for name, (x, _, _) in want.items()})
+
+
+def _logit_rows(name: str, t):
+    """Address, distance of the rows in elements and type of logits [B, n, vocab]."""
+    import torch
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}; [B, n, vocab] float32 or bfloat16, tokens side by side, is wanted")
+    stride = t.stride(1) if t.shape[1] > 1 else t.stride(0) if t.shape[0] > 1 else t.shape[2]
+    if t.shape[0] > 1 and t.stride(0) != stride * t.shape[1]:
+        raise ValueError(f"{name}: rows of all agents and nodes must be equally far apart")
+    _on_current_device(name, t)
+    return t.data_ptr(), stride, EN_F32 if t.dtype == torch.float32 else EN_BF16
+
+
+def token_rules_apply(rules: TokenRules, logits, out, parent=None, tokens=None, stream=None):
+    """logits, out: [B, n, vocab] float32 or bfloat16 (out may be logits); parent, tokens int32 [B, n] or both None."""
+    import torch
+    b, n, vocab = logits.shape
+    at, stride, dtype = _logit_rows("logits", logits)
+    to, out_stride, out_dtype = _logit_rows("out", out)
+    if out.shape != logits.shape or out_dtype != dtype:
+        raise ValueError(f"out: {tuple(out.shape)} {out.dtype} for logits {tuple(logits.shape)} {logits.dtype}")
+    rules.check(b, n, vocab)
+    ints = (torch.int32,)
+    _check(load().token_rules_apply(
+        rules.address, b, n, vocab, dtype, None if parent is None else _shaped("parent", parent, (b, n), ints),
+        None if tokens is None else _shaped("tokens", tokens, (b, n), ints), at, stride, to, out_stride, _stream(stream)))
+    return out
+
+
+def tree_accept_workspace_bytes(plan: Plan, n_nodes: int, vocab: int) -> int:
+    return int(load().en_tree_accept_workspace_bytes(plan.handle, int(n_nodes), int(vocab)))
+
+
+def token_tree_accept(plan: Plan, done, parent, tokens, logits, choice, path, n_accepted, next_token, done_out, ws=None,
+                      rules: Optional[TokenRules] = None, stream=None):
+    """done, n_accepted, next_token, done_out int32 [B]; parent, tokens, choice, path int32 [B, n]; logits [B, n, vocab]
+    float32 or bfloat16, or None: choice holds the choices. choice may be None with logits, done_out may be done."""
+    import torch
+    ints = (torch.int32,)
+    b, n = parent.shape
+    if b != plan.n_agents:
+        raise ValueError(f"parent: {b} agents, the plan has {plan.n_agents}")
+    at, stride, dtype, vocab, wsp, wsb = None, 0, EN_F32, 0, None, 0
+    if logits is not None:
+        at, stride, dtype = _logit_rows("logits", logits)
+        vocab = int(logits.shape[2])
+        if logits.shape[0] != b or logits.shape[1] != n:
+            raise ValueError(f"logits: {tuple(logits.shape)} for {b} agents and {n} nodes")
+        if rules is not None:
+            rules.check(b, n, vocab)
+        wsp, wsb = _room("ws", ws, 0)
+    _check(load().token_tree_accept(
+        plan.handle, rules.address if rules is not None else None, n, vocab, dtype, _shaped("done", done, (b,), ints),
+        _shaped("parent", parent, (b, n), ints), _shaped("tokens", tokens, (b, n), ints), at, stride,
+        None if choice is None else _shaped("choice", choice, (b, n), ints), _shaped("path", path, (b, n), ints),
+        _shaped("n_accepted", n_accepted, (b,), ints), _shaped("next_token", next_token, (b,), ints),
+        _shaped("done_out", done_out, (b,), ints), wsp, wsb, _stream(stream)))
+    return path, n_accepted, next_token
+
+
+def segmented_tree_commit(pool: Pool, plan: Plan, done, n_accepted, path, k_rows, v_rows, kc, vt, stream=None):
+    """done (after the acceptance), n_accepted int32 [B], path int32 [B, n]; k_rows, v_rows: a tensor [B, n, Hkv, D] per
+    layer, kc, vt: a context buffer per layer."""
+    import torch
+    d, ints, types = pool.desc, (torch.int32,), _torch_types(pool.desc)
+    b, n = path.shape
+    if b != plan.n_agents:
+        raise ValueError(f"path: {b} agents, the plan has {plan.n_agents}")
+    layers = len(k_rows)
+    if not layers == len(v_rows) == len(kc) == len(vt):
+        raise ValueError(f"{layers}, {len(v_rows)}, {len(kc)}, {len(vt)} layers")
+    shape, ctx, ptrs = (b, n, d.n_kv_heads, d.head_dim), context_bytes(pool, plan), C.c_void_p * layers
+    _check(load().segmented_tree_commit(
+        pool.handle, plan.handle, n, layers, _shaped("done", done, (b,), ints), _shaped("n_accepted", n_accepted, (b,), ints),
+        _shaped("path", path, (b, n), ints), ptrs(*[_shaped("k_rows", x, shape, types) for x in k_rows]),
+        ptrs(*[_shaped("v_rows", x, shape, types) for x in v_rows]), ptrs(*[_room("kc", x, ctx)[0] for x in kc]),
+        ptrs(*[_room("vt", x, ctx)[0] for x in vt]), _stream(stream)))
 
 
 class Tier:

@@ -890,6 +890,14 @@ static inline const int32_t *d_bnd(const en_plan *pl) { return d_sel(pl) + pl->s
 static inline const int32_t *d_hdr(const en_plan *pl) { return d_bnd(pl) + pl->bnd.size(); }
 static inline const int32_t *d_order(const en_plan *pl) { return d_hdr(pl) + pl->hdr.size(); }
 
+int en_ready_on_device(en_pool *pool, en_plan *plan, void *stream)
+{
+    const int rc = pool_ensure_device(pool);
+    return rc != EN_OK ? rc : plan_ensure_device(plan, (hipStream_t)stream);
+}
+const int32_t *en_plan_headers(const en_plan *plan) { return d_hdr(plan); }
+float en_softmax_scale_log2e(const en_pool *pool) { return softmax_scale_log2e(pool); }
+
 // ---------------------------------------------------------------------------
 // sizes
 // ---------------------------------------------------------------------------
@@ -998,6 +1006,18 @@ static void timing_release(en_pool *pool)
     pool->ev_start.clear();
     pool->ev_stop.clear();
     pool->ev_used = 0;
+}
+
+bool en_timing_begin(en_pool *pool, void *stream)
+{
+    if (pool->ev_used >= (int)pool->ev_start.size())
+        return false;
+    (void)hipEventRecord(pool->ev_start[pool->ev_used], (hipStream_t)stream);
+    return true;
+}
+void en_timing_end(en_pool *pool, void *stream)
+{
+    (void)hipEventRecord(pool->ev_stop[pool->ev_used++], (hipStream_t)stream);
 }
 
 static int en_timing_enable_impl(en_pool *pool, int32_t max_records)
@@ -1341,12 +1361,10 @@ static int run_attention(en_pool *pool, en_plan *plan, const void *q_dev, const 
     const bool fixed_point = mass_red_out_dev && ws && !red_direct && !few && mass_workgroups(pool, n_rows) <= EN_MASS_ARRIVALS;
     a.red_zero = fixed_point ? reinterpret_cast<unsigned long long *>(ws + L.redacc_off) : nullptr;
     a.n_red_zero = fixed_point ? plan->B * (plan->Smax + 1) : 0;
-    const bool timed = pool->ev_used < (int)pool->ev_start.size();
-    if (timed)
-        (void)hipEventRecord(pool->ev_start[pool->ev_used], (hipStream_t)stream);
+    const bool timed = en_timing_begin(pool, stream);
     int e = en_launch_attention(pool, a, stream);
     if (timed)
-        (void)hipEventRecord(pool->ev_stop[pool->ev_used++], (hipStream_t)stream);
+        en_timing_end(pool, stream);
     if (e != 0)
         return hip_fail((hipError_t)e, who);
     if (n_partials > 1) {

@@ -286,6 +286,43 @@ struct EnCtxAppendArgs {
     int B, Hkv, n, T, q_first;
 };
 
+// Decoding with drafted tokens (en_tree_host.cpp, en_tree.hip, en_tokens.hip).
+struct EnTreeArgs {
+    const void *q, *k_rows, *v_rows, *kc, *vt;
+    void *out;
+    const float *cos_tab, *sin_tab;
+    const int32_t *hdr, *done, *parent;
+    int B, Hq, Hkv, Nq, n, T;
+    float scale_log2e;
+};
+
+struct EnTreeCommitArgs {
+    const float *cos_tab, *sin_tab;
+    const int32_t *hdr, *done, *accepted, *path;
+    int B, Hkv, Nq, n, T, layers;
+    const void *k_rows[EN_TREE_COMMIT_LAYERS], *v_rows[EN_TREE_COMMIT_LAYERS];
+    void *kc[EN_TREE_COMMIT_LAYERS], *vt[EN_TREE_COMMIT_LAYERS];
+};
+
+struct EnRulesArgs {
+    en_token_rules rules;
+    const int32_t *parent, *tokens;
+    const void *logits;
+    void *out;                     // token_rules_apply
+    long long logits_stride, out_stride;
+    int B, n, vocab, chunks;
+    unsigned long long *best;      // token_tree_accept: [B, n, chunks]
+};
+constexpr int EN_RULES_CHUNK = 2048;      // tokens per workgroup
+
+struct EnAcceptArgs {
+    const int32_t *done, *parent, *tokens;
+    const unsigned long long *best;        // [B, n, chunks], or null: choice_in
+    const int32_t *choice_in;
+    int32_t *choice_out, *path, *accepted, *next, *done_out;
+    int B, n, Nq, chunks;
+};
+
 // Workspace layout helper (bytes, every part 256-byte aligned).
 struct EnWsLayout {
     size_t ml_off, seg_off, redacc_off, mlfin_off, opart_off, parts_off, total;
@@ -309,6 +346,11 @@ int en_launch_cluster(const en_pool *pool, const EnClusterArgs &a, void *stream)
 int en_launch_ctx_append(const en_pool *pool, const EnCtxAppendArgs &a, void *stream);
 int en_launch_mass(const en_pool *pool, const EnMassArgs &a, int reduce, void *stream);
 int en_launch_tier_load(const EnTierLoadArgs &a, int max_tokens, void *stream);
+int en_launch_tree_attention(const en_pool *pool, const EnTreeArgs &a, void *stream);
+int en_launch_tree_commit(const en_pool *pool, const EnTreeCommitArgs &a, void *stream);
+int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream);
+int en_launch_choices(const EnRulesArgs &a, int dtype, void *stream);
+int en_launch_accept(const EnAcceptArgs &a, void *stream);
 
 // The static device scratch of segmented_decode_step_static (en_static_scratch.hip,
 // EN_STATIC_SCRATCH_BYTES of the public header): the device address of the current device's copy
@@ -319,6 +361,14 @@ int en_launch_ceiling_mfma(float *sink_dev, int n_workgroups, int iters, int con
 int en_launch_ceiling_read(const void *src_dev, size_t bytes, void *sink_dev, int n_workgroups, void *stream);
 
 void en_set_error(const char *fmt, ...);
+
+// For entry points outside en_host.cpp: the pool's rotary table and the plan's block on the device (an en_status), the
+// plan's headers there, the factor of the scores, the measurement aid around a launch.
+int en_ready_on_device(en_pool *pool, en_plan *plan, void *stream);
+const int32_t *en_plan_headers(const en_plan *plan);
+float en_softmax_scale_log2e(const en_pool *pool);
+bool en_timing_begin(en_pool *pool, void *stream);
+void en_timing_end(en_pool *pool, void *stream);
 
 // Every extern "C" entry point that returns a status runs its body through this: no C++
 // exception (std::bad_alloc from a container sized by caller input, above all) crosses the C ABI.

@@ -1,0 +1,215 @@
+"""Attention over trees of drafted tokens (segmented_tree_attention) against the float64 oracle, which goes along each
+node's way by itself. Tolerances: tree_cases.near."""
+import numpy as np
+import pytest
+
+from tree_cases import TREES, Tree, chain, comb, near
+
+pytestmark = pytest.mark.gpu
+
+
+def check(t, layer=0):
+    import torch
+    got = t.attend(layer)
+    torch.cuda.synchronize()
+    near(got.float().cpu().numpy(), t.expected(layer), t.f32)
+
+
+def forest(agents, n, kinds=("comb", "chain", "broken", "star")):
+    return [TREES[kinds[b % len(kinds)]](n) for b in range(agents)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 16, 31, 33, 64])
+def test_nodes(dtype, d, n):
+    check(Tree(n, dtype, [200, 77, 0, 129], [3, 0, 1, 5], 80, forest(4, n), r=2, kv=2, d=d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r,kv,n,d", [(1, 1, 1, 64), (1, 3, 5, 128), (3, 2, 11, 64), (4, 8, 8, 128), (7, 1, 13, 128), (8, 2, 64, 64),
+                                      (7, 2, 64, 128), (16, 1, 4, 128), (32, 1, 1, 128), (5, 1, 40, 64), (20, 1, 64, 128)])
+def test_heads(dtype, r, kv, n, d):
+    check(Tree(r + n, dtype, [300, 65], [2, 7], 90, forest(2, n), r=r, kv=kv, d=d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("length", [0, 1, 15, 16, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 193, 255, 256, 257, 320, 511, 513, 1000, 2047])
+def test_lengths(dtype, length):
+    check(Tree(length, dtype, [length, max(0, length - 40)], [0, 17], 40, forest(2, 6), r=4, kv=1, d=128 if length % 2 else 64))
+
+
+@pytest.mark.parametrize("dtype,r,kv,n,d,lens", [("bf16", 4, 2, 8, 128, [9000]), ("bf16", 7, 1, 64, 128, [5000, 100]),
+                                                 ("bf16", 2, 1, 3, 64, [20000, 12000, 1]), ("f32", 2, 1, 9, 64, [6000, 33]),
+                                                 ("f32", 1, 1, 2, 128, [4000]), ("bf16", 1, 4, 64, 64, [3500, 3000])])
+def test_long_contexts(dtype, r, kv, n, d, lens):
+    check(Tree(n, dtype, lens, [5 * b for b in range(len(lens))], 100, forest(len(lens), n), r=r, kv=kv, d=d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("agents", [33, 150])
+def test_many_agents(dtype, agents):
+    rng = np.random.default_rng(agents)
+    check(Tree(agents, dtype, rng.integers(0, 400, agents), rng.integers(0, 9, agents), 20, forest(agents, 5), r=2, kv=2, d=64))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_absent_nodes_idle_agents_and_the_reserve(dtype):
+    """Rows without a node are zero, whatever their inputs hold; nodes that the reserve has no room for are absent."""
+    n = 12
+    done = [-1, 31, 2**31 - 1, -2**31, 30, 25, 0, 29]          # N_q = 30: idle x 4, full, 5 left, all left, one left
+    t = Tree(1, dtype, [100] * 8, done, 30, [chain(n)] * 6 + [np.full(n, -2), comb(n)], d=64)
+    want = t.expected()
+    assert not want[:5].any() and want[5, :5].any() and not want[5, 5:].any() and not want[6].any() and want[7, 0].any()
+    gone = (want == 0).all((2, 3))
+    for x in (t.q, t.k, t.v):
+        x[0][gone] = np.nan
+    t.up()
+    import torch
+    got = t.attend()
+    torch.cuda.synchronize()
+    got = got.float().cpu().numpy()
+    near(got, want, t.f32)
+    assert not got[gone].any()
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [9, 40])
+def test_rows_that_are_no_numbers_reach_their_descendants_only(dtype, value, n):
+    """A drafted token's rows of NaN or infinity: nodes beside it are what they are without it."""
+    t = Tree(n, dtype, [130, 50], [1, 0], 70, [comb(n), comb(n)], r=3, kv=1)
+    want = t.expected()
+    t.k[0][0, 4, 0, 5] = value
+    t.v[0][1, 5, 0, ::3] = value
+    t.up()
+    import torch
+    got = t.attend()
+    torch.cuda.synchronize()
+    got = got.float().cpu().numpy()
+    from oracle import tree
+    for b, bad in ((0, 4), (1, 5)):
+        ways = tree.ways(t.parent[b])
+        clean = [i for i in range(n) if bad not in ways[i]]
+        dirty = [i for i in range(n) if bad in ways[i]]
+        near(got[b, clean], want[b, clean], t.f32)
+        if b == 1:
+            # an infinite value with a weight above 0 is infinite, NaN is NaN; the other dimensions are as they were
+            assert not np.isfinite(got[b][dirty][..., ::3]).any()
+            rest = np.arange(t.d) % 3 != 0
+            near(got[b, dirty][..., rest], want[b, dirty][..., rest], t.f32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_context_rows_behind_the_last_token_are_not_looked_at(dtype):
+    a = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=np.nan)
+    b = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=np.inf)
+    c = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=0.0)
+    import torch
+    outs = [t.attend() for t in (a, b, c)]
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_scores(dtype):
+    """Scores of several hundred, from both sides, in the context and in the tree."""
+    t = Tree(8, dtype, [300, 10], [0, 4], 40, forest(2, 10), r=2, kv=1, d=64)
+    t.q *= 64.0
+    t.up()
+    import torch
+    got = t.attend()
+    torch.cuda.synchronize()
+    got, want = got.float().cpu().numpy(), t.expected()
+    assert np.isfinite(got).all()
+    if t.f32:
+        # scores of +-800: 2^-24 of them, a few times over, is 1e-4 of a weight
+        assert np.abs(got - want).max() <= 1e-3 * np.abs(want).max()
+    else:
+        # a rounded query's score is off by 64 * 0.02 (see near): weights by factors, outputs stay within the values
+        assert np.abs(got).max() <= np.abs(t.values[0][np.isfinite(t.values[0])]).max() + np.abs(t.v).max()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("n", [1, 5, 16])
+def test_a_chain_is_a_decode_step(dtype, d, n):
+    """With parent i - 1 the rows are those of segmented_decode_step(q_first = done)."""
+    import torch
+    from paper_2510_18546_amd import binding as B
+    t = Tree(n, dtype, [333, 333], [4, 4], 40, [chain(n)] * 2, r=2, kv=2, d=d, fill=0.0)
+    got = t.attend()
+    step = torch.empty_like(got)
+    ws = torch.empty(max(256, B.decode_workspace_bytes(t.pool, t.plan, n)), dtype=torch.uint8, device="cuda:0")
+    B.segmented_decode_step(t.pool, t.plan, 4, t.dq[0], t.dk[0], t.dv[0], t.kc[0], t.vt[0], step, ws)
+    torch.cuda.synchronize()
+    near(got.float().cpu().numpy(), t.expected(), t.f32)
+    near(step.float().cpu().numpy(), t.expected(), t.f32)
+
+
+def test_an_8_bit_pool_has_bf16_contexts():
+    import torch
+    from paper_2510_18546_amd import binding as B
+    t = Tree(3, "bf16", [150, 20], [2, 0], 30, forest(2, 8), d=128)
+    want = t.attend()
+    cap = 150
+    pool = B.kv_pool_create(None, None, t.lens, t.hq, 500000.0, cap + 30, dtype=B.EN_I8, k_ptr=t.block.data_ptr(),
+                            v_ptr=t.block.data_ptr(), shape=(2, t.kv, cap, t.d))
+    plan = B.segment_select(pool, [0, 1], [0, 1, 2], 30)
+    out = torch.empty_like(want)
+    ws = torch.empty(max(256, B.tree_workspace_bytes(pool, plan, 8)), dtype=torch.uint8, device="cuda:0")
+    B.segmented_tree_attention(pool, plan, t.ddone, t.dparent, t.dq[0], t.dk[0], t.dv[0], t.kc[0], t.vt[0], out, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_twice_the_same_bits_and_another_stream(dtype):
+    import torch
+    t = Tree(9, dtype, [1500, 700], [3, 8], 60, forest(2, 20), r=4, kv=2, d=128)
+    first = t.attend()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = t.attend()
+    torch.cuda.synchronize()
+    assert torch.equal(first, second)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_and_replayed(dtype):
+    """What changes from step to step is device memory: the graph follows it."""
+    import torch
+    t = Tree(4, dtype, [400, 90, 10], [0, 2, 5], 60, forest(3, 10), r=2, kv=2, d=64, fill=0.0)
+    out = t.attend()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        t.attend(out=out)
+    for step in range(4):
+        done = np.array([step, 7 * step - 1, 20], np.int32)
+        parent = np.stack(forest(3, 10, [("chain", "comb", "star", "broken")[(step + k) % 4] for k in range(3)])).astype(np.int32)
+        t.ddone.copy_(t.device(done))
+        t.dparent.copy_(t.device(parent))
+        out.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.float().cpu().numpy()
+        eager = t.attend()
+        torch.cuda.synchronize()
+        assert np.array_equal(got, eager.float().cpu().numpy())
+        t.done, t.parent = done, parent
+        near(got, t.expected(), t.f32)
+
+
+def test_timed_like_the_other_attention_calls():
+    import torch
+    from paper_2510_18546_amd import binding as B
+    t = Tree(2, "bf16", [200], [0], 20, [comb(6)])
+    B.timing_enable(t.pool, 4)
+    t.attend()
+    t.attend()
+    torch.cuda.synchronize()
+    ms = B.timing_collect(t.pool, 4)
+    assert len(ms) == 2 and (ms > 0).all()
