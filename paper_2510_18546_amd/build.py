@@ -19,6 +19,8 @@ SOURCES = [os.path.join(_CSRC, f) for f in
             "en_merge_mass.hip", "en_static_scratch.hip", "en_ceilings.hip", "en_tree_host.cpp", "en_tree.hip", "en_tokens.hip")]
 HEADERS = [os.path.join(_CSRC, "en_internal.h"), os.path.join(_CSRC, "en_device.h"), os.path.join(_CSRC, "en_tree_lane.h"),
            os.path.join(_ROOT, "include", "efficientnav.h")]
+# logits may be NaN, which is never the best token: comparisons there say what they say
+EXTRA_FLAGS = {"en_tokens.hip": ["-fhonor-nans"]}
 OBJ_DIR = os.path.join(_HERE, "_build")
 
 HIPCC_FLAGS = [
@@ -61,7 +63,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     inc = ["-I", os.path.join(_ROOT, "include"), "-I", _CSRC]
     objs = [os.path.join(OBJ_DIR, os.path.basename(src) + ".o") for src in SOURCES]
-    jobs = [[hipcc()] + HIPCC_FLAGS + inc + ["-c", src, "-o", obj] for src, obj in zip(SOURCES, objs)]
+    jobs = [[hipcc()] + HIPCC_FLAGS + EXTRA_FLAGS.get(os.path.basename(src), []) + inc + ["-c", src, "-o", obj]
+            for src, obj in zip(SOURCES, objs)]
     with ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 1)) as pool:
         errs = list(pool.map(_run, jobs))
     errs.append(_run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB_PATH]))

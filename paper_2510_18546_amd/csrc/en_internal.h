@@ -294,7 +294,14 @@ struct EnTreeArgs {
     const int32_t *hdr, *done, *parent;
     int B, Hq, Hkv, Nq, n, T;
     float scale_log2e;
+    int n_splits, n_ptiles;        // of an agent's key tiles; of the r * n query rows of a KV head
+    unsigned n_units;              // B * Hkv * n_splits * n_ptiles
+    EnDivisor by_ptiles, by_splits, by_hkv, by_n, by_hq;
+    float *ws_ml;                  // [n_splits, B * Hq * n, 2] (reference in log2 units, sum)
+    float *ws_opart;               // [n_splits, B * Hq * n, D] the splits' sums of values, not divided by their weights
 };
+// Row blocks of 32 (bf16) that a workgroup of the tree attention takes, one per wave.
+constexpr int EN_TREE_BLOCKS = 8;
 
 struct EnTreeCommitArgs {
     const float *cos_tab, *sin_tab;
@@ -346,7 +353,8 @@ int en_launch_cluster(const en_pool *pool, const EnClusterArgs &a, void *stream)
 int en_launch_ctx_append(const en_pool *pool, const EnCtxAppendArgs &a, void *stream);
 int en_launch_mass(const en_pool *pool, const EnMassArgs &a, int reduce, void *stream);
 int en_launch_tier_load(const EnTierLoadArgs &a, int max_tokens, void *stream);
-int en_launch_tree_attention(const en_pool *pool, const EnTreeArgs &a, void *stream);
+int en_launch_tree_attention(const en_pool *pool, const EnTreeArgs &a, int blocks, void *stream);
+int en_launch_tree_merge(const en_pool *pool, const EnTreeArgs &a, void *stream);
 int en_launch_tree_commit(const en_pool *pool, const EnTreeCommitArgs &a, void *stream);
 int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream);
 int en_launch_choices(const EnRulesArgs &a, int dtype, void *stream);

@@ -2,8 +2,10 @@
 // logits, acceptance, and the accepted tokens' way into the contexts of all layers.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 
 #include "en_internal.h"
 
@@ -46,11 +48,46 @@ static int check_nodes(int32_t n_nodes, const char *who)
 // ---------------------------------------------------------------------------
 // attention
 // ---------------------------------------------------------------------------
+// How a step of n nodes is cut: row blocks of a workgroup, workgroups over the rows of a KV head, splits of its keys.
+struct TreeCut {
+    int blocks, n_ptiles, n_splits;
+};
+static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
+{
+    TreeCut c{1, 1, 1};
+    if (pool->d.dtype == EN_F32)
+        return c;
+    const int all = (pool->r * n + EN_ROWS_PER_WAVE - 1) / EN_ROWS_PER_WAVE;
+    while (c.blocks < EN_TREE_BLOCKS && c.blocks < all)
+        c.blocks *= 2;
+    c.n_ptiles = (all + c.blocks - 1) / c.blocks;
+    const long units = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
+    const int tiles = (plan->max_ctx_len + EN_KEY_TILE - 1) / EN_KEY_TILE + 1;
+    const long slots = long(pool->n_cu) * (c.blocks == 8 ? 1 : 2) * 128 / pool->d.head_dim;
+    c.n_splits = int(std::max<long>(1, std::min<long>(std::min<long>(slots / std::max<long>(1, units), tiles), EN_MAX_SPLITS)));
+    if (const char *e = getenv("EN_TREE_SPLITS"))
+        c.n_splits = std::min(std::min(atoi(e), tiles), 64);
+    return c;
+}
+struct TreeWs {
+    size_t opart_off, total;
+};
+static TreeWs tree_ws(const en_pool *pool, const en_plan *plan, int n, int n_splits)
+{
+    TreeWs w{0, 0};
+    if (n_splits > 1) {
+        const size_t parts = size_t(n_splits) * plan->B * pool->d.n_q_heads * n;
+        w.opart_off = (parts * 2 * sizeof(float) + 255) & ~size_t(255);
+        w.total = w.opart_off + parts * pool->d.head_dim * sizeof(float);
+    }
+    return w;
+}
+
 extern "C" size_t en_tree_workspace_bytes(const en_pool *pool, const en_plan *plan, int32_t n_nodes)
 {
     if (!pool || !plan || n_nodes < 1 || n_nodes > EN_TREE_MAX_NODES)
         return 0;
-    return 0;
+    return tree_ws(pool, plan, n_nodes, tree_cut(pool, plan, n_nodes).n_splits).total;
 }
 
 static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n_nodes, const int32_t *done_dev,
@@ -78,11 +115,16 @@ static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n
         return fail(EN_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 (agent, head, node) rows", who);
     if (size_t(plan->ctx_stride) * pool->d.head_dim * elem > 0x7fffffffu)
         return fail(EN_ERR_UNSUPPORTED, "%s: a context of more than 2^31 - 1 bytes per KV head", who);
-    const size_t need = en_tree_workspace_bytes(pool, plan, n_nodes);
+    const TreeCut cut = tree_cut(pool, plan, n_nodes);
+    const TreeWs ws = tree_ws(pool, plan, n_nodes, cut.n_splits);
+    const size_t need = ws.total;
     if (need && !ws_dev)
         return fail(EN_ERR_INVALID_ARG, "%s: workspace of %zu bytes required", who, need);
     if (ws_bytes < need)
         return fail(EN_ERR_CAPACITY, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+    const size_t units = size_t(plan->B) * pool->d.n_kv_heads * cut.n_ptiles * cut.n_splits;
+    if (units > EN_GRID_MAX / 2)
+        return fail(EN_ERR_UNSUPPORTED, "%s: a step of %zu workgroups", who, units);
     if ((rc = en_ready_on_device(pool, plan, stream)) != EN_OK)
         return rc;
     EnTreeArgs a;
@@ -104,11 +146,23 @@ static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n
     a.n = n_nodes;
     a.T = plan->ctx_stride;
     a.scale_log2e = en_softmax_scale_log2e(pool);
+    a.n_splits = cut.n_splits;
+    a.n_ptiles = cut.n_ptiles;
+    a.n_units = unsigned(units);
+    a.by_ptiles = en_divisor(unsigned(cut.n_ptiles));
+    a.by_splits = en_divisor(unsigned(cut.n_splits));
+    a.by_hkv = en_divisor(unsigned(a.Hkv));
+    a.by_n = en_divisor(unsigned(n_nodes));
+    a.by_hq = en_divisor(unsigned(a.Hq));
+    a.ws_ml = need ? static_cast<float *>(ws_dev) : nullptr;
+    a.ws_opart = need ? reinterpret_cast<float *>(static_cast<char *>(ws_dev) + ws.opart_off) : nullptr;
     const bool timed = en_timing_begin(pool, stream);
-    const int e = en_launch_tree_attention(pool, a, stream);
+    const int e = en_launch_tree_attention(pool, a, cut.blocks, stream);
     if (timed)
         en_timing_end(pool, stream);
-    return launched(e, who);
+    if (e != 0 || cut.n_splits == 1)
+        return launched(e, who);
+    return launched(en_launch_tree_merge(pool, a, stream), "segmented_tree_attention merge");
 }
 extern "C" int segmented_tree_attention(en_pool *pool, en_plan *plan, int32_t n_nodes, const int32_t *done_dev,
                                         const int32_t *parent_dev, const void *q_dev, const void *k_rows_dev,
