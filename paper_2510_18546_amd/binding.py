@@ -6,6 +6,7 @@ of any kind: a missing library raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 import sys
@@ -216,8 +217,15 @@ class Pool:
 
 class Plan:
     def __init__(self, handle, pool: Pool, n_agents: int = 1):
-        self.handle, self.pool, self.n_agents = handle, pool, n_agents
+        self.handle, self.pool, self.n_agents, self._context_bytes = handle, pool, n_agents, None
         pool._plans.add(self)
+
+    @property
+    def context_bytes(self) -> int:
+        """Bytes of a context buffer; fixed when the plan is made."""
+        if self._context_bytes is None:
+            self._context_bytes = context_bytes(self.pool, self)
+        return self._context_bytes
 
     @property
     def info(self) -> PlanInfo:
@@ -434,85 +442,101 @@ def segmented_decode_step_static(pool: Pool, plan: Plan, q_first: int, q, k_rows
     return out
 
 
-def _shaped(name: str, t, shape, dtypes):
-    """A contiguous tensor of the current device, of that shape and one of these types; its address."""
-    if t.shape != shape or t.dtype not in dtypes or not t.is_contiguous():
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}{'' if t.is_contiguous() else ', not contiguous'}; "
-                         f"a contiguous {tuple(shape)} of {' or '.join(str(x) for x in dtypes)} is wanted")
-    _on_current_device(name, t)
+def _unfit(name: str, t, want: str) -> ValueError:
+    return ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+                      f"{want} on the current device is wanted")
+
+
+_get_device = None
+
+
+def _device() -> int:
+    """Launches go to the current device: a tensor elsewhere would be read there by address."""
+    global _get_device
+    if _get_device is None:
+        import torch
+        if not torch.cuda.is_available():
+            raise ValueError("drafted tokens are tensors on a GPU, and there is none")
+        torch.cuda.current_device()          # sets the device up if nothing has yet
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _get_device()
+
+
+def _at(name: str, t, shape, dtype, dev: int) -> int:
+    """Address of a contiguous tensor of that shape and type on the device."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev:
+        raise _unfit(name, t, f"a contiguous {tuple(shape)} of {dtype}")
     return t.data_ptr()
 
 
-_current_device = None
+def _buffer(name: str, t, nbytes: int, dev: int) -> int:
+    """Address of a buffer of at least `nbytes` on the device."""
+    if t.nbytes < nbytes or not t.is_contiguous() or t.get_device() != dev:
+        raise _unfit(name, t, f"a contiguous buffer of {nbytes} bytes")
+    return t.data_ptr()
 
 
-def _on_current_device(name: str, t):
-    """Launches go to the current device: a tensor elsewhere would be read there by address."""
-    global _current_device
-    if not t.is_cuda:
-        raise ValueError(f"{name}: on {t.device}, not on a GPU")
-    if _current_device is None:
+def _all_at(name: str, ts, nbytes: int, dtype, dev: int, exact: bool) -> array.array:
+    """Addresses of the layers' tensors, contiguous, of (`exact`) or of at least that many bytes, on the device."""
+    t_ = _torch().Tensor
+    sizes = list(map(t_.nbytes.__get__, ts))
+    if (min(sizes) < nbytes or exact and (max(sizes) != nbytes or any(t.dtype is not dtype for t in ts)) or
+            not all(map(t_.is_contiguous, ts)) or set(map(t_.get_device, ts)) != {dev}):
+        raise ValueError(f"{name}: a contiguous tensor of {'' if exact else 'at least '}{nbytes} bytes{f' of {dtype}' if exact else ''} on "
+                         "the current device is wanted for every layer")
+    return array.array("Q", map(t_.data_ptr, ts))
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
         import torch
-        torch.cuda.current_device()          # sets the device up if nothing has yet
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    if t.get_device() != _current_device():
-        raise ValueError(f"{name}: on {t.device}, not on the current device")
+        _torch_module = torch
+    return _torch_module
 
 
-def _torch_types(desc: PoolDesc):
-    import torch
-    return (torch.float32,) if desc.dtype == EN_F32 else (torch.bfloat16,)
+def _row_type(desc: PoolDesc):
+    return _torch().float32 if desc.dtype == EN_F32 else _torch().bfloat16
 
 
 def tree_workspace_bytes(pool: Pool, plan: Plan, n_nodes: int) -> int:
     return int(load().en_tree_workspace_bytes(pool.handle, plan.handle, int(n_nodes)))
 
 
-def _room(name: str, t, nbytes: int):
-    """Address and bytes of a buffer of at least `nbytes` on the current device."""
-    have = t.numel() * t.element_size()
-    if have < nbytes or not t.is_contiguous():
-        raise ValueError(f"{name}: {have} bytes, {nbytes} contiguous ones are wanted")
-    _on_current_device(name, t)
-    return t.data_ptr(), have
-
-
 def segmented_tree_attention(pool: Pool, plan: Plan, done, parent, q, k_rows, v_rows, kc, vt, out, ws=None, stream=None):
     """done int32 [B], parent int32 [B, n]; q, out [B, n, Hq, D], k_rows/v_rows [B, n, Hkv, D] in the contexts' type."""
-    import torch
-    d, n, ints = pool.desc, int(q.shape[1]), (torch.int32,)
-    b, types, ctx = int(q.shape[0]), _torch_types(d), context_bytes(pool, plan)
+    lib, i32, t, dev, d = load(), _torch().int32, _row_type(pool.desc), _device(), pool.desc
+    b, n = parent.shape
     if b != plan.n_agents:
-        raise ValueError(f"q: {b} agents, the plan has {plan.n_agents}")
-    rows, mine = (b, n, d.n_q_heads, d.head_dim), (b, n, d.n_kv_heads, d.head_dim)
-    wsp, wsb = _room("ws", ws, 0) if ws is not None else (None, 0)
-    _check(load().segmented_tree_attention(
-        pool.handle, plan.handle, n, _shaped("done", done, (b,), ints), _shaped("parent", parent, (b, n), ints),
-        _shaped("q", q, rows, types), _shaped("k_rows", k_rows, mine, types), _shaped("v_rows", v_rows, mine, types),
-        _room("kc", kc, ctx)[0], _room("vt", vt, ctx)[0], _shaped("out", out, rows, types), wsp, wsb, _stream(stream)))
+        raise ValueError(f"parent: {b} agents, the plan has {plan.n_agents}")
+    rows, mine, ctx = (b, n, d.n_q_heads, d.head_dim), (b, n, d.n_kv_heads, d.head_dim), plan.context_bytes
+    _check(lib.segmented_tree_attention(
+        pool.handle, plan.handle, n, _at("done", done, (b,), i32, dev), _at("parent", parent, (b, n), i32, dev),
+        _at("q", q, rows, t, dev), _at("k_rows", k_rows, mine, t, dev), _at("v_rows", v_rows, mine, t, dev),
+        _buffer("kc", kc, ctx, dev), _buffer("vt", vt, ctx, dev), _at("out", out, rows, t, dev),
+        _buffer("ws", ws, 0, dev) if ws is not None else None, ws.nbytes if ws is not None else 0, _stream(stream)))
     return out
 
 
 class TokenRules:
     """Rules on logits; keeps their tensors alive. See token_rules."""
 
-    def __init__(self, struct: _TokenRules, tensors: dict):
+    def __init__(self, struct: _TokenRules, tensors: list):
         self.struct, self.tensors = struct, tensors
         self.address = C.addressof(struct)
 
-    def check(self, n_agents: int, n_nodes: int, vocab: int):
-        t = self.tensors
-        words = (vocab + 31) // 32
-        for name, x in t.items():
-            if x is None:
-                continue
-            _on_current_device(name, x)
-            if x.shape[0] != n_agents and not (name == "bias" and x.dim() == 1):
-                raise ValueError(f"{name}: {tuple(x.shape)} for {n_agents} agents")
-        if t["bias"] is not None and t["bias"].shape[-1] < vocab:
-            raise ValueError(f"bias: {tuple(t['bias'].shape)} for {vocab} tokens")
-        if t["mask"] is not None and (t["mask"].shape[1] not in (1, n_nodes) or t["mask"].shape[2] < words):
-            raise ValueError(f"mask: {tuple(t['mask'].shape)} for {n_nodes} nodes and {words} words")
+    def check(self, n_agents: int, n_nodes: int, vocab: int, dev: int):
+        """The rules fit logits [n_agents, n_nodes, vocab] on that device."""
+        for name, x in self.tensors:
+            if x.get_device() != dev or x.shape[0] != n_agents and not (name == "bias" and x.dim() == 1):
+                raise _unfit(name, x, f"one for {n_agents} agents")
+            if name == "bias" and x.shape[-1] < vocab:
+                raise _unfit(name, x, f"one for {vocab} tokens")
+            if name == "mask" and (x.shape[1] not in (1, n_nodes) or 32 * x.shape[2] < vocab):
+                raise _unfit(name, x, f"one for {n_nodes} nodes and {vocab} tokens")
 
 
 def token_rules(penalties=None, history=None, history_len=None, bias=None, mask=None) -> TokenRules:
@@ -534,34 +558,40 @@ def token_rules(penalties=None, history=None, history_len=None, bias=None, mask=
                     mask.shape[1] * mask.shape[2] if mask is not None else 0,
                     mask.shape[2] if mask is not None and mask.shape[1] > 1 else 0,
                     history.shape[1] if history is not None else 0, 0)
-    return TokenRules(s, {name: x for name, (x, _, _) in want.items()})
+    return TokenRules(s, [(name, x) for name, (x, _, _) in want.items() if x is not None])
 
 
-def _logit_rows(name: str, t):
+def _logit_rows(name: str, t, dev: int):
     """Address, distance of the rows in elements and type of logits [B, n, vocab]."""
-    import torch
-    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or t.stride(2) != 1 and t.shape[2] > 1:
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}; [B, n, vocab] float32 or bfloat16, tokens side by side, is wanted")
-    stride = t.stride(1) if t.shape[1] > 1 else t.stride(0) if t.shape[0] > 1 else t.shape[2]
-    if t.shape[0] > 1 and t.stride(0) != stride * t.shape[1]:
-        raise ValueError(f"{name}: rows of all agents and nodes must be equally far apart")
-    _on_current_device(name, t)
-    return t.data_ptr(), stride, EN_F32 if t.dtype == torch.float32 else EN_BF16
+    if t.dtype is _torch().bfloat16:
+        dtype = EN_BF16
+    elif t.dtype is _torch().float32:
+        dtype = EN_F32
+    else:
+        raise _unfit(name, t, "float32 or bfloat16")
+    if t.dim() != 3 or t.get_device() != dev:
+        raise _unfit(name, t, "[B, n, vocab]")
+    b, n, vocab = t.shape
+    of_agent, stride, of_token = t.stride()
+    if n == 1:
+        stride = of_agent if b > 1 else vocab
+    if of_token != 1 and vocab > 1 or b > 1 and of_agent != n * stride:
+        raise _unfit(name, t, "[B, n, vocab] with tokens side by side and all rows equally far apart")
+    return t.data_ptr(), stride, dtype
 
 
 def token_rules_apply(rules: TokenRules, logits, out, parent=None, tokens=None, stream=None):
     """logits, out: [B, n, vocab] float32 or bfloat16 (out may be logits); parent, tokens int32 [B, n] or both None."""
-    import torch
+    lib, i32, dev = load(), _torch().int32, _device()
+    at, stride, dtype = _logit_rows("logits", logits, dev)
+    to, out_stride, _ = _logit_rows("out", out, dev)
+    if out.shape != logits.shape or out.dtype is not logits.dtype:
+        raise _unfit("out", out, f"{tuple(logits.shape)} of {logits.dtype}")
     b, n, vocab = logits.shape
-    at, stride, dtype = _logit_rows("logits", logits)
-    to, out_stride, out_dtype = _logit_rows("out", out)
-    if out.shape != logits.shape or out_dtype != dtype:
-        raise ValueError(f"out: {tuple(out.shape)} {out.dtype} for logits {tuple(logits.shape)} {logits.dtype}")
-    rules.check(b, n, vocab)
-    ints = (torch.int32,)
-    _check(load().token_rules_apply(
-        rules.address, b, n, vocab, dtype, None if parent is None else _shaped("parent", parent, (b, n), ints),
-        None if tokens is None else _shaped("tokens", tokens, (b, n), ints), at, stride, to, out_stride, _stream(stream)))
+    rules.check(b, n, vocab, dev)
+    _check(lib.token_rules_apply(
+        rules.address, b, n, vocab, dtype, None if parent is None else _at("parent", parent, (b, n), i32, dev),
+        None if tokens is None else _at("tokens", tokens, (b, n), i32, dev), at, stride, to, out_stride, _stream(stream)))
     return out
 
 
@@ -573,46 +603,46 @@ def token_tree_accept(plan: Plan, done, parent, tokens, logits, choice, path, n_
                       rules: Optional[TokenRules] = None, stream=None):
     """done, n_accepted, next_token, done_out int32 [B]; parent, tokens, choice, path int32 [B, n]; logits [B, n, vocab]
     float32 or bfloat16, or None: choice holds the choices. choice may be None with logits, done_out may be done."""
-    import torch
-    ints = (torch.int32,)
-    b, n = parent.shape
+    lib, i32, dev = load(), _torch().int32, _device()
+    b, n = tree = parent.shape
     if b != plan.n_agents:
         raise ValueError(f"parent: {b} agents, the plan has {plan.n_agents}")
-    at, stride, dtype, vocab, wsp, wsb = None, 0, EN_F32, 0, None, 0
+    at, stride, dtype, vocab, agents = None, 0, EN_F32, 0, (b,)
     if logits is not None:
-        at, stride, dtype = _logit_rows("logits", logits)
-        vocab = int(logits.shape[2])
-        if logits.shape[0] != b or logits.shape[1] != n:
-            raise ValueError(f"logits: {tuple(logits.shape)} for {b} agents and {n} nodes")
+        at, stride, dtype = _logit_rows("logits", logits, dev)
+        vocab = logits.shape[2]
+        if logits.shape[:2] != tree:
+            raise _unfit("logits", logits, f"[{b}, {n}, vocab]")
         if rules is not None:
-            rules.check(b, n, vocab)
-        wsp, wsb = _room("ws", ws, 0)
-    _check(load().token_tree_accept(
-        plan.handle, rules.address if rules is not None else None, n, vocab, dtype, _shaped("done", done, (b,), ints),
-        _shaped("parent", parent, (b, n), ints), _shaped("tokens", tokens, (b, n), ints), at, stride,
-        None if choice is None else _shaped("choice", choice, (b, n), ints), _shaped("path", path, (b, n), ints),
-        _shaped("n_accepted", n_accepted, (b,), ints), _shaped("next_token", next_token, (b,), ints),
-        _shaped("done_out", done_out, (b,), ints), wsp, wsb, _stream(stream)))
+            rules.check(b, n, vocab, dev)
+    _check(lib.token_tree_accept(
+        plan.handle, rules.address if rules is not None else None, n, vocab, dtype, _at("done", done, agents, i32, dev),
+        _at("parent", parent, tree, i32, dev), _at("tokens", tokens, tree, i32, dev), at, stride,
+        None if choice is None else _at("choice", choice, tree, i32, dev), _at("path", path, tree, i32, dev),
+        _at("n_accepted", n_accepted, agents, i32, dev), _at("next_token", next_token, agents, i32, dev),
+        _at("done_out", done_out, agents, i32, dev), _buffer("ws", ws, 0, dev) if ws is not None else None,
+        ws.nbytes if ws is not None else 0, _stream(stream)))
     return path, n_accepted, next_token
 
 
 def segmented_tree_commit(pool: Pool, plan: Plan, done, n_accepted, path, k_rows, v_rows, kc, vt, stream=None):
     """done (after the acceptance), n_accepted int32 [B], path int32 [B, n]; k_rows, v_rows: a tensor [B, n, Hkv, D] per
     layer, kc, vt: a context buffer per layer."""
-    import torch
-    d, ints, types = pool.desc, (torch.int32,), _torch_types(pool.desc)
+    lib, i32, dev, d, t = load(), _torch().int32, _device(), pool.desc, _row_type(pool.desc)
     b, n = path.shape
     if b != plan.n_agents:
         raise ValueError(f"path: {b} agents, the plan has {plan.n_agents}")
     layers = len(k_rows)
     if not layers == len(v_rows) == len(kc) == len(vt):
         raise ValueError(f"{layers}, {len(v_rows)}, {len(kc)}, {len(vt)} layers")
-    shape, ctx, ptrs = (b, n, d.n_kv_heads, d.head_dim), context_bytes(pool, plan), C.c_void_p * layers
-    _check(load().segmented_tree_commit(
-        pool.handle, plan.handle, n, layers, _shaped("done", done, (b,), ints), _shaped("n_accepted", n_accepted, (b,), ints),
-        _shaped("path", path, (b, n), ints), ptrs(*[_shaped("k_rows", x, shape, types) for x in k_rows]),
-        ptrs(*[_shaped("v_rows", x, shape, types) for x in v_rows]), ptrs(*[_room("kc", x, ctx)[0] for x in kc]),
-        ptrs(*[_room("vt", x, ctx)[0] for x in vt]), _stream(stream)))
+    if layers == 0:
+        return
+    mine, ctx = b * n * d.n_kv_heads * d.head_dim * t.itemsize, plan.context_bytes
+    ptrs = [_all_at("k_rows", k_rows, mine, t, dev, True), _all_at("v_rows", v_rows, mine, t, dev, True),
+            _all_at("kc", kc, ctx, t, dev, False), _all_at("vt", vt, ctx, t, dev, False)]
+    _check(lib.segmented_tree_commit(
+        pool.handle, plan.handle, n, layers, _at("done", done, (b,), i32, dev), _at("n_accepted", n_accepted, (b,), i32, dev),
+        _at("path", path, (b, n), i32, dev), *(p.buffer_info()[0] for p in ptrs), _stream(stream)))
 
 
 class Tier:

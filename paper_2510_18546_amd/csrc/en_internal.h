@@ -318,9 +318,10 @@ struct EnRulesArgs {
     void *out;                     // token_rules_apply
     long long logits_stride, out_stride;
     int B, n, vocab, chunks;
+    int nodes;                     // rows of an agent that a workgroup takes
     unsigned long long *best;      // token_tree_accept: [B, n, chunks]
 };
-constexpr int EN_RULES_CHUNK = 2048;      // tokens per workgroup
+constexpr int EN_RULES_CHUNK = 4096;      // tokens per workgroup
 
 struct EnAcceptArgs {
     const int32_t *done, *parent, *tokens;

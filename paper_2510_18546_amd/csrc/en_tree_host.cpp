@@ -266,6 +266,13 @@ static int check_logits(int32_t vocab, int32_t dtype, const void *p, int64_t str
         return fail(EN_ERR_INVALID_ARG, "%s: logits not aligned to an element", who);
     return EN_OK;
 }
+// Rows of an agent that a workgroup takes.
+static int rules_nodes(const EnRulesArgs &a)
+{
+    const long want = (a.rules.penalties_dev ? 4 : 16) * 256;
+    const long groups = std::min<long>(a.n, std::max<long>(1, want / (long(a.B) * a.chunks)));
+    return int((a.n + groups - 1) / groups);
+}
 static int chunks_of(int32_t vocab) { return int((int64_t(vocab) + EN_RULES_CHUNK - 1) / EN_RULES_CHUNK); }
 
 static int token_rules_apply_impl(const en_token_rules *rules, int32_t n_agents, int32_t n_nodes, int32_t vocab,
@@ -297,6 +304,7 @@ static int token_rules_apply_impl(const en_token_rules *rules, int32_t n_agents,
     a.vocab = vocab;
     a.chunks = chunks_of(vocab);
     a.best = nullptr;
+    a.nodes = rules_nodes(a);
     return launched(en_launch_rules(a, dtype, stream), who);
 }
 extern "C" int token_rules_apply(const en_token_rules *rules, int32_t n_agents, int32_t n_nodes, int32_t vocab, int32_t dtype,
@@ -359,6 +367,7 @@ static int token_tree_accept_impl(const en_plan *plan, const en_token_rules *rul
         c.vocab = vocab;
         c.chunks = chunks_of(vocab);
         c.best = static_cast<unsigned long long *>(ws_dev);
+        c.nodes = rules_nodes(c);
         if ((rc = launched(en_launch_choices(c, dtype, stream), who)) != EN_OK)
             return rc;
         a.best = c.best;
