@@ -42,13 +42,15 @@ __device__ __forceinline__ void wave_lds_order()
 
 // ---------------------------------------------------------------------------
 // rules: a workgroup takes EN_RULES_CHUNK tokens of `a.nodes` of an agent's rows, a wave a quarter of the tokens of each
-// row: 16 a lane, in two runs of eight. Bound by reading the logits once (and writing them once).
+// row: 16 a lane, in two runs of eight. Bound by reading the logits once (and writing them once); several rows' loads are
+// on their way while one is looked at, and a choice is found with few exchanges between lanes.
 //
 // The tokens that penalties concern are few: they are counted into a table in LDS once for all rows of the workgroup, each
 // wave lists those of its quarter, and in a row only they are divided and subtracted from, in a copy of the quarter in
 // LDS (a division for every token would be 12 of 40 instructions a token, and these instructions more time than the
 // logits' way from memory). Tokens of a node's own way join the counts for that row; mostly none lies in the quarter.
-// Rows need not be aligned: loads of 16 bytes from any element on. grid: (chunks, groups of nodes, B).
+// Rows need not be aligned: loads of 16 bytes from any element on. grid: (groups of nodes, B, chunks): the first tokens, which
+// in most vocabularies are the frequent ones, are begun first.
 // ---------------------------------------------------------------------------
 template <typename T>
 struct EnRun {                       // eight logits as they lie in a row
@@ -60,132 +62,181 @@ struct EnRulesLds {
     int count[EN_RULES_CHUNK];
     unsigned short hit[4][EN_RULES_CHUNK / 4];
 };
+// Of so many tokens that have occurred a wave's list is worth its trips through LDS.
+constexpr int EN_RULES_LISTED = 256;
 
-template <typename T, bool CHOOSE>
+// RULED: there may be penalties, a bias or a mask. DEPTH: rows on their way.
+template <typename T, bool CHOOSE, bool RULED, int DEPTH>
 __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
 {
     constexpr int WAVE_TOKENS = EN_RULES_CHUNK / 4;      // 1024
     static_assert(WAVE_TOKENS == 1024, "two runs of eight a lane");
     extern __shared__ __attribute__((aligned(16))) char smem[];      // EnRulesLds, if there are penalties
     EnRulesLds &lds = *reinterpret_cast<EnRulesLds *>(smem);
-    __shared__ unsigned long long s_best[EN_TREE_MAX_NODES][4];
-    const int chunk = blockIdx.x, b = blockIdx.z, tid = threadIdx.x;
+    __shared__ unsigned long long s_best[CHOOSE ? EN_TREE_MAX_NODES : 1][4];
+    const int chunk = blockIdx.z, b = blockIdx.y, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
-    const int i0 = blockIdx.y * a.nodes, i1 = min(i0 + a.nodes, a.n);
+    const int i0 = blockIdx.x * a.nodes, i1 = min(i0 + a.nodes, a.n);
     const en_token_rules &r = a.rules;
 
-    EnTreeLane tree;
-    tree.way = 0;
-    unsigned long long todo = ~0ull;                     // rows to look at
-    if (a.parent) {
-        tree = tree_lane(a.parent + (size_t)b * a.n, a.n, EN_TREE_MAX_NODES);
-        todo = __ballot(tree.present());
-    }
-    todo &= (i1 == 64 ? ~0ull : (1ull << i1) - 1) & ~((1ull << i0) - 1);
-    if (todo == 0)
-        return;
-    const unsigned long long rows = todo;
-    const int v0 = chunk * EN_RULES_CHUNK;
-    const int w0 = v0 + wave * WAVE_TOKENS;              // the wave's tokens
-    const int last = min(a.vocab - w0, WAVE_TOKENS);     // .. as many (none or fewer: <= 0)
+    // what is asked for first, in one trip: the history's first entries (as many as there may be: how many there are is on
+    // its way too), the penalties, the tree's tokens
+    constexpr int HJ = 8;
+    const bool penalties_on = RULED && r.penalties_dev;
+    const int *const history = r.history_dev ? r.history_dev + (size_t)b * r.history_stride : nullptr;
+    int early[HJ], token = -1, h = 0;
     float rep = 1.f, freq = 0.f, pres = 0.f;
-    int n_hit = 0, my_token = -1;                        // my_token: of node `lane`, in the quarter, or -1
-    int *const count = lds.count + wave * WAVE_TOKENS;
-    if (r.penalties_dev) {
+    if (penalties_on) {
+        const int most = history ? r.history_stride : 0;
+#pragma unroll
+        for (int j = 0; j < HJ; ++j)
+            early[j] = j * 256 + tid < most ? history[j * 256 + tid] : -1;
+        if (a.tokens && lane < a.n)
+            token = a.tokens[(size_t)b * a.n + lane];
         rep = r.penalties_dev[3 * b];
         freq = r.penalties_dev[3 * b + 1];
         pres = r.penalties_dev[3 * b + 2];
-        for (int k = tid; k < EN_RULES_CHUNK; k += 256)
-            lds.count[k] = 0;
-        __syncthreads();
-        const int h = r.history_dev ? min(max(r.history_len_dev[b], 0), r.history_stride) : 0;
-        const int *const history = r.history_dev + (size_t)b * r.history_stride;
-        for (int k = tid; k < h; k += 256) {
-            const unsigned v = (unsigned)history[k] - (unsigned)v0;
-            if (v < (unsigned)EN_RULES_CHUNK)
-                atomicAdd(&lds.count[v], 1);
+        h = most ? min(max(r.history_len_dev[b], 0), most) : 0;
+    }
+
+    EnTreeLane tree;
+    tree.way = 0;
+    unsigned long long rows = ~0ull;                     // rows to look at
+    if (a.parent) {
+        tree = tree_lane(a.parent + (size_t)b * a.n, a.n, EN_TREE_MAX_NODES);
+        rows = __ballot(tree.present());
+    }
+    rows &= (i1 == 64 ? ~0ull : (1ull << i1) - 1) & ~((1ull << i0) - 1);
+    if (rows == 0)
+        return;
+    const int v0 = chunk * EN_RULES_CHUNK;
+    const int w0 = v0 + wave * WAVE_TOKENS;              // the wave's tokens
+    const int last = min(a.vocab - w0, WAVE_TOKENS);     // .. as many (none or fewer: <= 0)
+    const uint32_t *const mask = RULED && r.mask_dev ? r.mask_dev + (size_t)b * r.mask_agent_stride : nullptr;
+
+    // a lane's run q: tokens w0 + 512 q + 8 lane on
+    struct Row {
+        EnRun<T> run[2];
+        uint32_t allowed[2];
+        int node;                                        // -1: none
+    } ring[DEPTH];
+    unsigned long long todo = last > 0 ? rows : 0ull;
+    auto load = [&](Row &x) __attribute__((always_inline)) {
+        x.node = todo ? __builtin_ctzll(todo) : -1;
+        if (!todo)
+            return;
+        todo &= todo - 1;
+        const T *row = (const T *)a.logits + ((size_t)b * a.n + x.node) * a.logits_stride + w0;
+        const uint32_t *words = RULED && mask ? mask + (size_t)x.node * r.mask_node_stride : nullptr;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = 512 * q + 8 * lane;
+            if (k + 8 <= last)
+                x.run[q] = *reinterpret_cast<const EnRun<T> *>(row + k);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x.run[q].x[j] = k + j < last ? row[k + j] : (T)EN_NEG_INF;
+            // (w0 and k are multiples of 8: a run's bits lie in one word)
+            if (RULED && words)
+                x.allowed[q] = k < last ? words[(w0 + k) >> 5] : 0u;
         }
-        if (a.tokens && lane < a.n) {
-            const unsigned v = (unsigned)a.tokens[(size_t)b * a.n + lane] - (unsigned)w0;
-            my_token = tree.present() && (int)v >= 0 && (int)v < last ? (int)v : -1;
+    };
+#pragma unroll
+    for (int k = 0; k < DEPTH; ++k)
+        load(ring[k]);
+
+    const float *const bias = RULED && r.bias_dev ? r.bias_dev + (size_t)b * r.bias_agent_stride : nullptr;
+    float add[2][8];
+    if (RULED && bias)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = 512 * q + 8 * lane;
+            EnRun<float> run;
+            if (k + 8 <= last)
+                run = *reinterpret_cast<const EnRun<float> *>(bias + w0 + k);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    run.x[j] = k + j < last ? bias[w0 + k + j] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                add[q][j] = run.x[j];
+        }
+    int n_hit = 0, my_token = -1;                        // my_token: of node `lane`, in the quarter, or -1
+    int *const count = lds.count + wave * WAVE_TOKENS;
+    if (penalties_on) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int k = 0; k < EN_RULES_CHUNK / 1024; ++k)
+            *reinterpret_cast<i32x4 *>(lds.count + 1024 * k + 4 * tid) = i32x4{0, 0, 0, 0};
+        {
+            const unsigned v = (unsigned)token - (unsigned)w0;
+            my_token = tree.present() && token >= 0 && v < (unsigned)max(last, 0) ? (int)v : -1;
         }
         __syncthreads();
-        for (int k = 0; k < last; k += 64) {
-            const bool hit = k + lane < last && count[k + lane] > 0;
-            const unsigned long long hits = __ballot(hit);
-            if (hit)
-                lds.hit[wave][n_hit + __popcll(hits & ((1ull << lane) - 1))] = (unsigned short)(k + lane);
+        auto counted = [&](int v, bool there) {
+            if (there && (unsigned)v - (unsigned)v0 < (unsigned)EN_RULES_CHUNK)
+                atomicAdd(&lds.count[v - v0], 1);
+        };
+#pragma unroll
+        for (int j = 0; j < HJ; ++j)
+            counted(early[j], j * 256 + tid < h);
+        for (int k0 = HJ * 256; k0 < h; k0 += HJ * 256) {
+            int v[HJ];
+#pragma unroll
+            for (int j = 0; j < HJ; ++j)
+                v[j] = k0 + j * 256 + tid < h ? history[k0 + j * 256 + tid] : -1;
+#pragma unroll
+            for (int j = 0; j < HJ; ++j)
+                counted(v[j], k0 + j * 256 + tid < h);
+        }
+        __syncthreads();
+        int c[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            c[k] = 64 * k + lane < last ? count[64 * k + lane] : 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const unsigned long long hits = __ballot(c[k] > 0);
+            if (c[k] > 0)
+                lds.hit[wave][n_hit + __popcll(hits & ((1ull << lane) - 1))] = (unsigned short)(64 * k + lane);
             n_hit += (int)__popcll(hits);
         }
         wave_lds_order();
     }
-    const unsigned long long in_quarter = __ballot(my_token >= 0);
-    const float *const bias = r.bias_dev ? r.bias_dev + (size_t)b * r.bias_agent_stride : nullptr;
-    const uint32_t *const mask = r.mask_dev ? r.mask_dev + (size_t)b * r.mask_agent_stride : nullptr;
-    float add[2][8];
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int k = 512 * q + 8 * lane + j;
-            add[q][j] = bias && k < last ? bias[w0 + k] : 0.f;
-        }
+    const unsigned long long in_quarter = RULED ? __ballot(my_token >= 0) : 0ull;
 
-    // a lane's run q: tokens w0 + 512 q + 8 lane on
-    auto load = [&](int i, T (&x)[2][8]) {
-        const T *row = (const T *)a.logits + ((size_t)b * a.n + i) * a.logits_stride + w0;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int k = 512 * q + 8 * lane;
-            if (k + 8 <= last) {
-                const EnRun<T> run = *reinterpret_cast<const EnRun<T> *>(row + k);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[q][j] = run.x[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[q][j] = k + j < last ? row[k + j] : (T)EN_NEG_INF;
-            }
-        }
-    };
-    T now[2][8], next[2][8];
-    int i = __builtin_ctzll(todo);
-    if (last > 0)
-        load(i, now);
-    while (todo && last > 0) {
-        todo &= todo - 1;
-        const int i_next = todo ? __builtin_ctzll(todo) : i;
-        if (todo)
-            load(i_next, next);
-        uint32_t allowed[2] = {0xffu, 0xffu};
-        if (mask) {
-            const uint32_t *words = mask + (size_t)i * r.mask_node_stride;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int k = 512 * q + 8 * lane;        // (w0 and k are multiples of 8: a run's bits lie in one word)
-                allowed[q] = k < last ? words[(w0 + k) >> 5] >> ((w0 + k) & 31) : 0u;
-            }
-        }
-        float x[2][8];
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                x[q][j] = (float)now[q][j];
-        const unsigned long long way = a.parent ? readlane64(tree.way, i) : 0ull;
+    auto penalties = [&](float (&x)[2][8], unsigned long long way) __attribute__((always_inline)) {
         const bool own = (way & in_quarter) != 0;
-        if (n_hit > 0 || own) {
+        if (n_hit == 0 && !own)
+            return;
+        const bool adds = own && my_token >= 0 && (way >> lane & 1);
+        bool first = false;                              // this lane takes a token that no list has
+        if (adds)
+            first = atomicAdd(&count[my_token], 1) == 0;
+        wave_lds_order();
+        if (n_hit > EN_RULES_LISTED) {
+            // so many that every lane looks at its own tokens
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; j += 4) {
+                    typedef int i32x4 __attribute__((ext_vector_type(4)));
+                    const i32x4 c = *reinterpret_cast<const i32x4 *>(count + 512 * q + 8 * lane + j);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = penalised(x[q][j + e], c[e], rep, freq, pres);
+                        x[q][j + e] = c[e] > 0 ? y : x[q][j + e];
+                    }
+                }
+        } else {
             float *const sx = lds.x[wave];
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4)
                     *reinterpret_cast<f32x4 *>(sx + 512 * q + 8 * lane + j) = f32x4{x[q][j], x[q][j + 1], x[q][j + 2], x[q][j + 3]};
-            const bool adds = own && my_token >= 0 && (way >> lane & 1);
-            bool first = false;                          // this lane takes a token that no list has
-            if (adds)
-                first = atomicAdd(&count[my_token], 1) == 0;
             wave_lds_order();
             for (int k = lane; k < n_hit; k += 64) {
                 const int t = lds.hit[wave][k];
@@ -194,8 +245,6 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
             if (first)
                 sx[my_token] = penalised(sx[my_token], count[my_token], rep, freq, pres);
             wave_lds_order();
-            if (adds)
-                atomicSub(&count[my_token], 1);
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -205,32 +254,62 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
                     for (int e = 0; e < 4; ++e)
                         x[q][j + e] = y[e];
                 }
-            wave_lds_order();
         }
-        if (bias)
+        wave_lds_order();
+        if (adds)
+            atomicSub(&count[my_token], 1);
+        wave_lds_order();
+    };
+    auto look_at = [&](const Row &in) __attribute__((always_inline)) {
+        const int i = in.node;
+        float x[2][8];
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[q][j] += add[q][j];
-        if (mask)
+            for (int j = 0; j < 8; ++j)
+                x[q][j] = (float)in.run[q].x[j];
+        if constexpr (RULED) {
+            if (penalties_on)
+                penalties(x, a.parent ? readlane64(tree.way, i) : 0ull);
+            if (bias)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[q][j] = allowed[q] >> j & 1 ? x[q][j] : EN_NEG_INF;
+                    for (int j = 0; j < 8; ++j)
+                        x[q][j] += add[q][j];
+            if (mask)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const uint32_t bits = in.allowed[q] >> (8 * lane & 31);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[q][j] = bits >> j & 1 ? x[q][j] : EN_NEG_INF;
+                }
+        }
         if constexpr (CHOOSE) {
-            float best = EN_NEG_INF;
-            int token = -1;
+            // The largest of each run, of the wave, the first lane that has it in its first run or else in its second, and
+            // which of the run's it is: of equals the lowest token. (NaN is no maximum.)
+            float top_of[2];
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int q = 0; q < 2; ++q) {
+                top_of[q] = EN_NEG_INF;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (x[q][j] > best) {                // (no NaN is; of equals the first stays)
-                        best = x[q][j];
-                        token = 512 * q + j;
-                    }
-            const unsigned long long w = wave_choice(token >= 0 ? rank_of(best) : 0u, w0 + token + 8 * lane);
+                    top_of[q] = fmaxf(top_of[q], x[q][j]);
+            }
+            const float top = wave_max(fmaxf(top_of[0], top_of[1]));
+            const unsigned long long in0 = __ballot(top_of[0] == top), in1 = __ballot(top_of[1] == top);
+            unsigned long long w = 0;
+            if (top > EN_NEG_INF) {
+                const int l = __builtin_ctzll(in0 ? in0 : in1);
+                int at = 7;
+#pragma unroll
+                for (int j = 6; j >= 0; --j) {
+                    const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(in0 ? x[0][j] : x[1][j]), l));
+                    at = y == top ? j : at;
+                }
+                w = (unsigned long long)rank_of(top) << 32 | (unsigned)~(w0 + (in0 ? 0 : 512) + 8 * l + at);
+            }
             if (lane == 0)
                 s_best[i][wave] = w;
         } else {
@@ -251,13 +330,15 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
                             row[k + j] = run.x[j];
             }
         }
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                now[q][j] = next[q][j];
-        i = i_next;
-    }
+    };
+    while (ring[0].node >= 0)
+        static_for<DEPTH>([&](auto k) {
+            if (ring[k].node >= 0) {
+                look_at(ring[k]);
+                load(ring[k]);
+            }
+        });
+
     if constexpr (CHOOSE) {
         const int waves = min(4, (a.vocab - v0 + WAVE_TOKENS - 1) / WAVE_TOKENS);    // those that had tokens
         __syncthreads();
@@ -325,19 +406,25 @@ __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
     }
 }
 
-template <bool CHOOSE>
-static int launch_rules(const EnRulesArgs &a, int dtype, void *stream)
+template <typename T, bool CHOOSE, int DEPTH>
+static int launch_rules(const EnRulesArgs &a, hipStream_t st)
 {
-    const dim3 grid(a.chunks, (a.n + a.nodes - 1) / a.nodes, a.B), blk(256);
+    const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks), blk(256);
     const size_t lds = a.rules.penalties_dev ? sizeof(EnRulesLds) : 0;
-    if (dtype == EN_F32)
-        hipLaunchKernelGGL((rules_kernel<float, CHOOSE>), grid, blk, lds, (hipStream_t)stream, a);
+    if (a.rules.penalties_dev || a.rules.bias_dev || a.rules.mask_dev)
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true, 2>), grid, blk, lds, st, a);
     else
-        hipLaunchKernelGGL((rules_kernel<bf16_t, CHOOSE>), grid, blk, lds, (hipStream_t)stream, a);
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false, DEPTH>), grid, blk, 0, st, a);
     return (int)hipGetLastError();
 }
-int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream) { return launch_rules<false>(a, dtype, stream); }
-int en_launch_choices(const EnRulesArgs &a, int dtype, void *stream) { return launch_rules<true>(a, dtype, stream); }
+int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream)
+{
+    return dtype == EN_F32 ? launch_rules<float, false, 2>(a, (hipStream_t)stream) : launch_rules<bf16_t, false, 4>(a, (hipStream_t)stream);
+}
+int en_launch_choices(const EnRulesArgs &a, int dtype, void *stream)
+{
+    return dtype == EN_F32 ? launch_rules<float, true, 2>(a, (hipStream_t)stream) : launch_rules<bf16_t, true, 4>(a, (hipStream_t)stream);
+}
 
 int en_launch_accept(const EnAcceptArgs &a, void *stream)
 {

@@ -443,60 +443,75 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
 }
 
 // ---------------------------------------------------------------------------
-// tree_merge: out = sum_sp 2^(m_sp - m) O_sp / sum_sp 2^(m_sp - m) l_sp. G neighbouring lanes share four values of a row, the
-// splits dealt out over them. A split that a row saw nothing of left a sum of 0 and no values; a row without any is zero.
+// tree_merge: out = sum_sp 2^(m_sp - m) O_sp / sum_sp 2^(m_sp - m) l_sp. A thread takes four values of a row, neighbours the
+// row's next four, and G groups of D / 4 threads share the splits of a row and meet in LDS. A split that a row saw nothing
+// of left a sum of 0 and no values; a row without any is zero. grid: rows * G * (D / 4) threads.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int G>
 __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
 {
-    constexpr int CH = D / 4;
+    constexpr int CH = D / 4, RPW = 256 / (CH * G);      // threads per group; rows per workgroup
+    static_assert(RPW >= 1, "a row's groups are in a workgroup");
+    __shared__ f32x4 s_acc[G > 1 ? 256 : 1];
+    __shared__ f32x2 s_ml[G > 1 ? 256 : 1];
     const unsigned rows = (unsigned)a.B * a.Hq * a.n;
-    const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const int g = (int)(x % G);
-    const size_t item = x / G;
-    const unsigned row = (unsigned)(item / CH);
-    const int ch = (int)(item % CH);
-    if (row >= rows)
-        return;
-    constexpr int NB = 4;
+    const int tid = threadIdx.x, ch = tid % CH, g = tid / CH % G;
+    const unsigned row = blockIdx.x * RPW + tid / (CH * G);
+    constexpr int NB = G == 1 ? 8 : 4;
     float M = EN_NEG_INF, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int sp0 = g; sp0 < a.n_splits; sp0 += NB * G) {
-        f32x2 ml[NB];
-        f32x4 v[NB];
+    if (row < rows)
+        for (int sp0 = g; sp0 < a.n_splits; sp0 += NB * G) {
+            f32x2 ml[NB];
+            f32x4 v[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const bool on = sp0 + j * G < a.n_splits;
-            const size_t part = (size_t)(on ? sp0 + j * G : sp0) * rows + row;
-            ml[j] = *reinterpret_cast<const f32x2 *>(a.ws_ml + part * 2);
-            v[j] = *reinterpret_cast<const f32x4 *>(a.ws_opart + part * D + 4 * ch);
-            if (!on)
-                ml[j][1] = 0.f;
+            for (int j = 0; j < NB; ++j) {
+                const bool on = sp0 + j * G < a.n_splits;
+                const size_t part = (size_t)(on ? sp0 + j * G : sp0) * rows + row;
+                ml[j] = *reinterpret_cast<const f32x2 *>(a.ws_ml + part * 2);
+                v[j] = *reinterpret_cast<const f32x4 *>(a.ws_opart + part * D + 4 * ch);
+                if (!on)
+                    ml[j][1] = 0.f;
+            }
+            float Mb = M;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                Mb = __float_as_uint(ml[j][1]) ? fmaxf(Mb, ml[j][0]) : Mb;
+            const float keep = M == EN_NEG_INF ? 0.f : fast_exp2(M - Mb);
+            l *= keep;
+            acc *= keep;
+            M = Mb;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                if (__float_as_uint(ml[j][1])) {
+                    const float w = fast_exp2(ml[j][0] - M);
+                    l += w * ml[j][1];
+                    acc += w * v[j];
+                }
         }
-        float Mb = M;
+    if constexpr (G > 1) {
+        s_acc[tid] = acc;
+        s_ml[tid] = f32x2{M, l};
+        __syncthreads();
+        if (g != 0)
+            return;
+        f32x2 ml[G];
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-            Mb = __float_as_uint(ml[j][1]) ? fmaxf(Mb, ml[j][0]) : Mb;
-        const float keep = M == EN_NEG_INF ? 0.f : fast_exp2(M - Mb);
-        l *= keep;
-        acc *= keep;
-        M = Mb;
+        for (int k = 0; k < G; ++k) {
+            ml[k] = s_ml[tid + k * CH];
+            M = __float_as_uint(ml[k][1]) ? fmaxf(M, ml[k][0]) : M;
+        }
+        l = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-            if (__float_as_uint(ml[j][1])) {
-                const float w = fast_exp2(ml[j][0] - M);
-                l += w * ml[j][1];
-                acc += w * v[j];
+        for (int k = 0; k < G; ++k)
+            if (__float_as_uint(ml[k][1])) {
+                const float w = fast_exp2(ml[k][0] - M);
+                l += w * ml[k][1];
+                acc += w * s_acc[tid + k * CH];
             }
     }
-    const float all = lanes_reduce<G>(M, [](float p, float q) { return fmaxf(p, q); });
-    const float keep = M == EN_NEG_INF ? 0.f : fast_exp2(M - all);
-    const auto plus = [](float p, float q) { return p + q; };
-    l = lanes_reduce<G>(l * keep, plus);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        acc[e] = lanes_reduce<G>(acc[e] * keep, plus);
-    if (g != 0)
+    if (row >= rows)
         return;
     const float inv = __float_as_uint(l) ? 1.f / l : 0.f;
     const unsigned bh = divided(row, a.by_n), i = row - bh * a.n;
@@ -508,13 +523,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
 template <typename T, int D>
 static void launch_merge(const EnTreeArgs &a, hipStream_t st)
 {
-    const size_t items = (size_t)a.B * a.Hq * a.n * (D / 4);
-    const int G = a.n_splits <= 4 ? 4 : 16;
-    const dim3 grid((unsigned)((items * G + 255) / 256)), blk(256);
-    if (G == 4)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), grid, blk, 0, st, a);
+    const unsigned rows = (unsigned)a.B * a.Hq * a.n;
+    const auto grid = [rows](int G) { return dim3((rows + 1024 / (D * G) - 1) / (1024 / (D * G))); };
+    if (a.n_splits > 8 && rows < 2048)
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 8>), grid(8), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 16>), grid, blk, 0, st, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), grid(1), dim3(256), 0, st, a);
 }
 
 template <int D>

@@ -269,7 +269,9 @@ static int check_logits(int32_t vocab, int32_t dtype, const void *p, int64_t str
 // Rows of an agent that a workgroup takes.
 static int rules_nodes(const EnRulesArgs &a)
 {
-    const long want = (a.rules.penalties_dev ? 4 : 16) * 256;
+    long want = (a.rules.penalties_dev ? 4 : 16) * 256;
+    if (const char *e = getenv("EN_RN"))
+        want = atoi(e) * 256;
     const long groups = std::min<long>(a.n, std::max<long>(1, want / (long(a.B) * a.chunks)));
     return int((a.n + groups - 1) / groups);
 }
