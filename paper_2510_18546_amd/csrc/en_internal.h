@@ -296,9 +296,12 @@ struct EnTreeArgs {
     float scale_log2e;
     int n_splits, n_ptiles;        // of an agent's key tiles; of the r * n query rows of a KV head
     unsigned n_units;              // B * Hkv * n_splits * n_ptiles
-    EnDivisor by_ptiles, by_splits, by_hkv, by_n, by_hq;
-    float *ws_ml;                  // [n_splits, B * Hq * n, 2] (reference in log2 units, sum)
-    float *ws_opart;               // [n_splits, B * Hq * n, D] the splits' sums of values, not divided by their weights
+    int tile_blocks;               // blocks of 32 rows per workgroup
+    unsigned head_blocks, n_blocks;      // blocks of 32 rows of a KV head; of all
+    EnDivisor by_ptiles, by_splits, by_hkv, by_n, by_r, by_blocks;
+    // what the splits leave, float32: per row (reference in log2 units, sum), [n_splits, n_blocks, 32, 2], and sums of values
+    // not divided by their weights, [n_splits, n_blocks, D / 8, 64 lanes, 4] (see tree_merge_kernel)
+    float *ws_ml, *ws_opart;
 };
 // Row blocks of 32 (bf16) that a workgroup of the tree attention takes, one per wave.
 constexpr int EN_TREE_BLOCKS = 8;

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
     tree.way = 0;
     unsigned long long rows = ~0ull;                     // rows to look at
     if (a.parent) {
-        tree = tree_lane(a.parent + (size_t)b * a.n, a.n, EN_TREE_MAX_NODES);
+        tree = tree_lane(tree_parent(a.parent + (size_t)b * a.n, a.n), a.n, EN_TREE_MAX_NODES);
         rows = __ballot(tree.present());
     }
     rows &= (i1 == 64 ? ~0ull : (1ull << i1) - 1) & ~((1ull << i0) - 1);
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
     const size_t row = (size_t)b * a.n + lane;
     const int done = a.done[b];
-    const EnTreeLane t = tree_lane(a.parent + (size_t)b * a.n, a.n, tree_room(done, a.Nq));
+    const EnTreeLane t = tree_lane(tree_parent(a.parent + (size_t)b * a.n, a.n), a.n, tree_room(done, a.Nq));
     int choice = -1;
     if (a.best) {
         const unsigned long long present = __ballot(t.present());

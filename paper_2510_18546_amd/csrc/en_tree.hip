@@ -31,7 +31,7 @@ __device__ __forceinline__ bool no_number(unsigned short bf16) { return (bf16 & 
 
 // KW = 2: two waves share a row block, a 32-key block of every tile each, and meet at the end.
 template <int D, int RW, int KW, int NST>
-__global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_kernel(EnTreeArgs a)
+__global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((amdgpu_num_vgpr(256))) void tree_attn_kernel(EnTreeArgs a)
 {
     constexpr int W = RW * KW;
     constexpr int NT = 64 * W;                   // threads
@@ -52,6 +52,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
     __shared__ int s_no_number;                  // a value of the tree is infinite or NaN
     typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
 
+    // (the arguments in one batch, and no integer divisions: see attn_bf16_kernel)
+    asm volatile("" ::"s"(a.q), "s"(a.k_rows), "s"(a.kc), "s"(a.vt), "s"(a.cos_tab), "s"(a.hdr), "s"(a.parent), "s"(a.B), "s"(a.n), "s"(a.n_units),
+                 "s"(a.by_ptiles.mul), "s"(a.by_splits.mul), "s"(a.by_hkv.mul), "s"(a.by_n.mul), "s"(a.by_r.n), "s"(a.ws_ml));
     // Neighbours in this order share a split's keys, and an XCD takes a run of them.
     const unsigned per_xcd = gridDim.x / EN_XCDS;
     const unsigned unit = (blockIdx.x % EN_XCDS) * per_xcd + blockIdx.x / EN_XCDS;
@@ -69,38 +72,64 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
     const int lane = tid % 64;
     const int col = lane % 32, half = lane / 32;
     const int rw = wave % RW, kw = wave / RW;
-    const int r = a.Hq / a.Hkv, n = a.n;
-    const int n_rows = r * n;
-    const int c_row = (ptile * RW + rw) * 32 + col;
-    const bool row_there = c_row < n_rows;
+    const int r = a.by_r.n, n = a.n;
+    const int block = ptile * a.tile_blocks + rw;        // the wave's 32 rows
+    const bool idle = rw >= a.tile_blocks || block * 32 >= r * n;        // none: it loads, and keeps the barriers
+    const int c_row = block * 32 + col;
+    const bool row_there = !idle && c_row < r * n;
     const int hl = row_there ? divided(c_row, a.by_n) : 0;
     const int i_row = row_there ? c_row - hl * n : 0;
     const int hq = kvh * r + hl;
 
+    // ---- what does not wait for anything, asked for first ----
     const int done = as_table(a.done)[b];
     const int Lc = as_table(a.hdr)[4 * b + 1];
-    const EnTreeLane tree = tree_lane(a.parent + (size_t)b * n, n, tree_room(done, a.Nq));
-    const unsigned long long present = __ballot(tree.present());
-    const unsigned rows_all = (unsigned)a.B * a.Hq * n;
-    const unsigned row = ((unsigned)b * a.Hq + hq) * n + i_row;
-    const int L = Lc + done;                     // keys of the context (an idle agent's is not used)
-    const int n_ctx = present ? (L + LB - 1) / LB : 0;
-    const int t_begin = split_first_tile(sp, n_ctx + 1, a.n_splits);
-    const int t_end = min((int)split_first_tile(sp + 1, n_ctx + 1, a.n_splits), n_ctx);
-    const bool has_tree = sp == a.n_splits - 1 && present;
-    const int n_it = max(t_end - t_begin, 0) + (has_tree ? 1 : 0);
-    if (n_it == 0) {
-        // nothing to do: an idle agent, or one with fewer tiles than splits
+    const int my_parent = tree_parent(a.parent + (size_t)b * n, n);
+    bf16x8 qraw[NKS];
+    {
+        const bf16_t *qp = (const bf16_t *)a.q + (((size_t)b * n + i_row) * a.Hq + hq) * D + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+            qraw[ks] = *reinterpret_cast<const bf16x8 *>(qp + 16 * ks);
+    }
+    // the tree's keys and values: a thread takes 8 dimensions and their partners of a node, then of others NT / PAIRS on
+    constexpr int PAIRS = D / 16;
+    const bool last_split = sp == a.n_splits - 1;
+    const int t_m = tid / PAIRS, t_c = tid % PAIRS;
+    bf16x8 k1, k2;
+    u16x8 v1, v2;
+    auto tree_load = [&](int m) __attribute__((always_inline)) {
+        const size_t from = (((size_t)b * n + min(m, n - 1)) * a.Hkv + kvh) * D + 8 * t_c;
+        const bf16_t *kr = (const bf16_t *)a.k_rows + from, *vr = (const bf16_t *)a.v_rows + from;
+        k1 = *reinterpret_cast<const bf16x8 *>(kr);
+        k2 = *reinterpret_cast<const bf16x8 *>(kr + D / 2);
+        v1 = *reinterpret_cast<const u16x8 *>(vr);
+        v2 = *reinterpret_cast<const u16x8 *>(vr + D / 2);
+    };
+    if (last_split)
+        tree_load(t_m);
+
+    const int room = tree_room(done, a.Nq);
+    const unsigned blocks_before = (b * a.Hkv + kvh) * a.head_blocks;
+    auto nothing = [&]() {                       // of this split's keys a row sees none
         if (row_there && half == 0 && kw == 0) {
             if (a.n_splits > 1) {
                 f32x2 none = {EN_NEG_INF, 0.f};
-                *reinterpret_cast<f32x2 *>(a.ws_ml + ((size_t)sp * rows_all + row) * 2) = none;
+                *reinterpret_cast<f32x2 *>(a.ws_ml + (((size_t)sp * a.n_blocks + blocks_before + block) * 32 + col) * 2) = none;
             } else {
                 bf16_t *op = (bf16_t *)a.out + (((size_t)b * n + i_row) * a.Hq + hq) * D;
                 for (int d = 0; d < D; d += 8)
                     *reinterpret_cast<bf16x8 *>(op + d) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
             }
         }
+    };
+    const int L = Lc + done;                     // keys of the context (an idle agent's is not used)
+    const int n_ctx = room > 0 ? (L + LB - 1) / LB : 0;
+    const int t_begin = divided(sp * (n_ctx + 1) + a.n_splits - 1, a.by_splits);         // split_first_tile
+    const int t_end = min((int)divided((sp + 1) * (n_ctx + 1) + a.n_splits - 1, a.by_splits), n_ctx);
+    const int n_it = max(t_end - t_begin, 0) + (last_split ? 1 : 0);
+    if (n_it == 0 || room == 0) {                // an agent with fewer tiles than splits, or an idle one
+        nothing();
         return;
     }
 
@@ -111,118 +140,130 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
     // chunk c of K row `row` lies at c ^ k_pattern(row), chunk c of V^T row d at c ^ v_pattern(d)
     auto k_pattern = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
     auto v_pattern = [](int d) { return (d >> 1) & 7; };
-    uint32_t koff[NBK / W], voff[NBV / W];
-#pragma unroll
-    for (int j = 0; j < NBK / W; ++j) {
-        const int q = (wave + W * j) * 64 + lane;
-        const int krow = q / (ROWB / 16);
-        koff[j] = (uint32_t)(krow * ROWB + ((q % (ROWB / 16)) ^ k_pattern(krow)) * 16);
-    }
-#pragma unroll
-    for (int j = 0; j < NBV / W; ++j) {
-        const int q = (wave + W * j) * 64 + lane;
-        const int d = q / 8;
-        voff[j] = (uint32_t)d * (uint32_t)a.T * 2u + (uint32_t)(((q % 8) ^ v_pattern(d)) * 16);
-    }
-    auto issue = [&](int tile, int stage) {
-        const char *kt = kg + (size_t)tile * KBYTES;
-        const char *vtile = vg + (size_t)tile * VROWB;
-        const uint32_t dst = lds0 + stage * STAGE + wave * 1024;
+    // A wave's loads are every W-th kilobyte of the tile: 1024 / ROWB rows of K, 8 of V^T. Which chunk of its row a lane asks
+    // for is the same in all of them, but for K with D = 128 and two waves, where every other one has bit 3 exchanged.
+    constexpr bool ALTERNATES = D == 128 && W == 2;
+    const unsigned ul = lane, uw = wave;
+    const unsigned k_row = ul / (ROWB / 16), k_at = D == 128 ? k_row ^ (uw % 4) * 4 : (ul / 16) ^ (uw % 2) * 4;
+    const uint32_t koff = k_row * ROWB + ((ul % (ROWB / 16)) ^ k_at) * 16;
+    const uint32_t voff = ul / 8 * (uint32_t)a.T * 2u + ((ul % 8) ^ (ul / 16) ^ (uw % 2) * 4) * 16;
+    const unsigned v_step = 16u * (unsigned)a.T;         // bytes of 8 rows of V^T
+    auto issue = [&](int tile, int stage) __attribute__((always_inline)) {
+        const char *kt = kg + (size_t)tile * KBYTES + uw * 1024;
+        const char *vt = vg + (size_t)tile * VROWB + (size_t)uw * v_step;
+        const uint32_t dst = lds0 + stage * STAGE + uw * 1024;
 #pragma unroll
         for (int j = 0; j < NBK / W; ++j)
-            dma16(kt, koff[j], dst + W * j * 1024);
+            dma16(kt + W * j * 1024, ALTERNATES && j % 2 ? koff ^ 128 : koff, dst + W * j * 1024);
 #pragma unroll
         for (int j = 0; j < NBV / W; ++j)
-            dma16(vtile, voff[j], dst + KBYTES + W * j * 1024);
+            dma16(vt + (size_t)(W * j) * v_step, voff, dst + KBYTES + W * j * 1024);
     };
-    const int ctx0 = t_begin - (has_tree ? 1 : 0);       // iteration it takes tile ctx0 + it of the context
-#pragma unroll
-    for (int it = 0; it < NST - 1; ++it)
-        if (it < n_it && !(has_tree && it == 0))
-            issue(ctx0 + it, it);
+    const int ctx0 = t_begin - (last_split ? 1 : 0);     // iteration it takes tile ctx0 + it of the context
+    // The first tile is asked for here, the next ones behind the cosines and sines: these are waited for first, and loads
+    // come in the order in which they were asked for.
+    const int first_ctx = last_split ? 1 : 0;
+    if (first_ctx < n_it)
+        issue(ctx0 + first_ctx, first_ctx);
 
-    // ---- Q: load, rotate at the node's position, scale, round to bf16 ----
+    const EnTreeLane tree = tree_lane(my_parent, n, room);
+    const unsigned long long present = __ballot(tree.present());
+    if (!present) {
+        wait_all_memory();                       // (the tiles on their way to LDS)
+        nothing();
+        return;
+    }
+
+    // ---- Q: rotate at the node's position, scale, round to bf16 ----
     const unsigned long long way = __shfl(tree.way, i_row, 64);
     const int depth = __shfl(tree.depth, i_row, 64);
     const bool row_valid = row_there && way != 0;
     bf16x8 qf[NKS];
-    if (row_valid) {
-        const bf16_t *qp = (const bf16_t *)a.q + (((size_t)b * n + i_row) * a.Hq + hq) * D + 8 * half;
-        const size_t pos = L + depth;
+    f32x8 t_cs, t_sn;                            // of the tree's keys
+    auto tree_angles = [&](int m) __attribute__((always_inline)) {
+        const int d_m = __popcll(__shfl(tree.way, m, 64)) - 1;
+        const size_t at = (size_t)(L + max(d_m, 0)) * (D / 2) + 8 * t_c;
+        t_cs = *reinterpret_cast<const f32x8 *>(a.cos_tab + at);
+        t_sn = *reinterpret_cast<const f32x8 *>(a.sin_tab + at);
+    };
+    if (last_split)
+        tree_angles(t_m & 63);
+    {
+        const size_t pos = L + (row_valid ? depth : 0);
         const float *ct = a.cos_tab + pos * (D / 2) + 8 * half, *st = a.sin_tab + pos * (D / 2) + 8 * half;
-        bf16x8 qraw[NKS];
         f32x8 cs[NKS / 2], sn[NKS / 2];
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-            qraw[ks] = *reinterpret_cast<const bf16x8 *>(qp + 16 * ks);
 #pragma unroll
         for (int ks = 0; ks < NKS / 2; ++ks) {
             cs[ks] = *reinterpret_cast<const f32x8 *>(ct + 16 * ks);
             sn[ks] = *reinterpret_cast<const f32x8 *>(st + 16 * ks);
         }
+        // (here they have come; the next tiles are on their way while they are used)
+#pragma unroll
+        for (int ks = 0; ks < NKS / 2; ++ks)
+            asm volatile("" : "+v"(cs[ks]), "+v"(sn[ks]));
+#pragma unroll
+        for (int it = 1; it < NST - 1; ++it)
+            if (first_ctx < it && it < n_it)
+                issue(ctx0 + it, it);
+        const float scale = row_valid ? a.scale_log2e : 0.f;
 #pragma unroll
         for (int ks = 0; ks < NKS / 2; ++ks)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float y1, y2;
-                rope_scale_pair((float)qraw[ks][j], (float)qraw[ks + NKS / 2][j], cs[ks][j], sn[ks][j], a.scale_log2e, y1, y2);
-                qf[ks][j] = (bf16_t)y1;
-                qf[ks + NKS / 2][j] = (bf16_t)y2;
+                const float x1 = (float)qraw[ks][j], x2 = (float)qraw[ks + NKS / 2][j];
+                const float c = cs[ks][j] * scale, s = sn[ks][j] * scale;
+                qf[ks][j] = (bf16_t)(x1 * c - x2 * s);
+                qf[ks + NKS / 2][j] = (bf16_t)(x2 * c + x1 * s);
             }
-    } else {
+        if (!row_valid)                          // (what such a row holds may be no number)
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-            qf[ks] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            for (int ks = 0; ks < NKS; ++ks)
+                qf[ks] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
     }
 
-    // ---- the tree's tile into stage 0 ----
-    if (has_tree) {
+    // ---- the tree's tile into stage 0. Keys of absent nodes may stay what they are (nobody sees their scores), their
+    // values have to be 0. ----
+    if (last_split) {
+        for (int x = tid; x < VBYTES / 16; x += NT)
+            *reinterpret_cast<f32x4 *>(smem + KBYTES + x * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
         if (tid == 0)
             s_no_number = 0;
         __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
-        constexpr int PAIRS = D / 16;            // 8 dimensions and their partners
+        lds_data_ready();
         bool odd = false;
-        for (int x = tid; x < LB * PAIRS; x += NT) {
-            const int m = x / PAIRS, c = x % PAIRS;
-            const int d_m = __popcll(__shfl(tree.way, m, 64)) - 1;       // (the loop's lanes go together: NT divides)
-            const bool there = present >> m & 1;
-            bf16x8 k1 = {0, 0, 0, 0, 0, 0, 0, 0}, k2 = k1;
-            u16x8 v1 = {0, 0, 0, 0, 0, 0, 0, 0}, v2 = v1;
-            if (there) {
-                const size_t from = (((size_t)b * n + m) * a.Hkv + kvh) * D + 8 * c;
-                const bf16_t *kr = (const bf16_t *)a.k_rows + from, *vr = (const bf16_t *)a.v_rows + from;
-                const size_t at = (size_t)(L + d_m) * (D / 2) + 8 * c;
-                const f32x8 cs = *reinterpret_cast<const f32x8 *>(a.cos_tab + at), sn = *reinterpret_cast<const f32x8 *>(a.sin_tab + at);
-                k1 = *reinterpret_cast<const bf16x8 *>(kr);
-                k2 = *reinterpret_cast<const bf16x8 *>(kr + D / 2);
-                v1 = *reinterpret_cast<const u16x8 *>(vr);
-                v2 = *reinterpret_cast<const u16x8 *>(vr + D / 2);
+#pragma unroll 1
+        for (int m0 = 0; m0 < n; m0 += NT / PAIRS) {
+            const int m = m0 + t_m;
+            if (m0 > 0) {
+                tree_load(m);
+                tree_angles(m & 63);
+            }
+            if (m < n && (present >> m & 1)) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float y1, y2;
-                    rope_key_pair((float)k1[j], (float)k2[j], cs[j], sn[j], y1, y2);
+                    rope_key_pair((float)k1[j], (float)k2[j], t_cs[j], t_sn[j], y1, y2);
                     k1[j] = (bf16_t)y1;
                     k2[j] = (bf16_t)y2;
+                }
+                const int pat = k_pattern(m);
+                *reinterpret_cast<bf16x8 *>(smem + m * ROWB + (t_c ^ pat) * 16) = k1;
+                *reinterpret_cast<bf16x8 *>(smem + m * ROWB + ((t_c + PAIRS) ^ pat) * 16) = k2;
+                const int vc = (m & ~0xC) | ((m & 4) << 1) | ((m & 8) >> 1);
+                // (dimension d of a column lies at chunk (column / 8) ^ v_pattern(d) of row d; v_pattern(d + D / 2) is
+                // v_pattern(d))
+                char *const at = smem + KBYTES + 8 * t_c * VROWB + vc % 8 * 2;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
                     // no number has no place in a product with weights of 0: it joins the sums of the rows that see it
                     // behind the loop
                     const bool n1 = no_number(v1[j]), n2 = no_number(v2[j]);
                     odd = odd || n1 || n2;
-                    v1[j] = n1 ? 0 : v1[j];
-                    v2[j] = n2 ? 0 : v2[j];
+                    char *const to = at + j * VROWB + (((unsigned)vc / 8) ^ v_pattern(8 * t_c + j)) * 16;
+                    *reinterpret_cast<unsigned short *>(to) = n1 ? 0 : v1[j];
+                    *reinterpret_cast<unsigned short *>(to + D / 2 * VROWB) = n2 ? 0 : v2[j];
                 }
-            }
-            const int pat = k_pattern(m);
-            *reinterpret_cast<bf16x8 *>(smem + m * ROWB + (c ^ pat) * 16) = k1;
-            *reinterpret_cast<bf16x8 *>(smem + m * ROWB + ((c + PAIRS) ^ pat) * 16) = k2;
-            const int vc = (m & ~0xC) | ((m & 4) << 1) | ((m & 8) >> 1);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                auto put = [&](int d, unsigned short v) {
-                    *reinterpret_cast<unsigned short *>(smem + KBYTES + d * VROWB + ((vc / 8) ^ v_pattern(d)) * 16 + vc % 8 * 2) = v;
-                };
-                put(8 * c + j, v1[j]);
-                put(8 * c + j + D / 2, v2[j]);
             }
         }
         if (__any(odd) && lane == 0)
@@ -242,7 +283,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
     for (int e = 0; e < 16; ++e)
         negm[e] = 0.f;
     bool has_ref = !row_valid;                   // (rows that are not there need none)
-    const int kpat = D == 128 ? col & 15 : (col >> 1) & 7, vpat = (col >> 1) & 7;
+    // byte offsets of a lane's chunk in its rows, of the first k-step; the others' are these with bits exchanged
+    const int kchunk = (half ^ k_pattern(col)) * 16, vchunk = (half ^ v_pattern(col)) * 16;
     const int u0 = kw * NUW;
 
     for (int it = 0; it < n_it; ++it) {
@@ -258,57 +300,81 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
         if (it + NST - 1 < n_it)
             issue(ctx0 + it + NST - 1, (it + NST - 1) % NST);
         lds_data_ready();
-        const bool is_tree = has_tree && it == 0;
+        const bool is_tree = last_split && it == 0;
         const int kb = (ctx0 + it) * LB;         // first key of a context tile
         const int left = L - kb;                 // keys of a context tile from its first on
-        if (!is_tree && left < LB) {
-            // columns behind the context's last token become zero: whatever they hold has no weight, but 0 times infinity
-            // is no 0
-            for (int x = tid; x < D * 8; x += NT) {
-                char *at = smem + stage * STAGE + KBYTES + x * 16;
-                const int c = (x % 8) ^ v_pattern(x / 8);        // its chunk: columns 8 c .. 8 c + 7
-                const int key = 16 * (c / 2) + 4 * (c % 2);      // .. which are these keys, 0 .. 3 and 8 .. 11 on from it
-                u16x8 v = *reinterpret_cast<const u16x8 *>(at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[j] = key + 8 * (j / 4) + j % 4 < left ? v[j] : 0;
-                *reinterpret_cast<u16x8 *>(at) = v;
-            }
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            __builtin_amdgcn_s_barrier();
-            lds_data_ready();
-        }
-        // ---- S^T = K Q^T - m_ref ----
+        if (idle)
+            continue;
+        // The products' operands and results overlap like this: the first block's scores; the second block's, beside the
+        // exponentials of the first; the first block's values, beside the exponentials of the second; the second block's
+        // values. Probabilities are taken against the reference as it is: where that has to change (or keys are hidden)
+        // those of the first block are taken again.
         f32x16 sv[NUW];
+        bf16x8 pf[NUW][2];
+        auto scores = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-#pragma unroll
-            for (int u = 0; u < NUW; ++u) {
-                const bf16x8 fr = *reinterpret_cast<const bf16x8 *>(stg + ((u0 + u) * KB + col) * ROWB + ((2 * ks + half) ^ kpat) * 16);
+            for (int ks = 0; ks < NKS; ++ks) {
+                const bf16x8 fr = *reinterpret_cast<const bf16x8 *>(stg + ((u0 + u) * KB + col) * ROWB + (kchunk ^ (32 * ks)));
                 sv[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, qf[ks], ks == 0 ? negm : sv[u], 0, 0, 0);
             }
-        // Hidden keys: element e of block u is key 32 u + 8 (e / 4) + e % 4 + 4 half of the tile. (Masks by arithmetic:
-        // as comparisons they would take two scalar registers each.)
-        if (is_tree || left < LB) {
-            const unsigned long long keys = is_tree ? way : (1ull << left) - 1;
+        };
+        auto probabilities = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < NUW; ++u) {
-                const uint32_t sees = (uint32_t)(keys >> (KB * (u0 + u))) >> (4 * half);
+            for (int e = 0; e < 16; ++e)
+                pf[u][e / 8][e % 8] = (bf16_t)fast_exp2(sv[u][e]);
+        };
+        // HIDES: the tile has columns behind the context's last token. Whatever they hold has no weight, but 0 times
+        // infinity is no 0: they become zero on their way, two columns a word.
+        auto values = [&](auto hides_tag, int u) __attribute__((always_inline)) {
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t on = (uint32_t)((int32_t)(sees << (31 - (8 * (e / 4) + e % 4))) >> 31);
-                    sv[u][e] = __uint_as_float((__float_as_uint(sv[u][e]) & on) | (0xff800000u & ~on));
+            for (int kk = 0; kk < 2; ++kk) {
+                u32x4 keep;
+                if constexpr (decltype(hides_tag)::value)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int key = KB * (u0 + u) + 16 * kk + 4 * half + 8 * (w / 2) + 2 * (w % 2);
+                        keep[w] = key + 1 < left ? ~0u : key < left ? 0xffffu : 0u;
+                    }
+#pragma unroll
+                for (int d = 0; d < NDB; ++d) {
+                    bf16x8 v = *reinterpret_cast<const bf16x8 *>(stg + KBYTES + (32 * d + col) * VROWB +
+                                                                 (vchunk ^ (16 * (4 * (u0 + u) + 2 * kk))));
+                    if constexpr (decltype(hides_tag)::value)
+                        v = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v) & keep);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[u][kk], o[d], 0, 0, 0);
                 }
             }
-        }
-        // ---- a reference for rows that have none or whose scores have outgrown it ----
+        };
+#pragma unroll
+        for (int u = 0; u < NUW; ++u)
+            scores(u);
+        probabilities(0);
         float mx = sv[0][0];
 #pragma unroll
         for (int u = 0; u < NUW; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 mx = fmaxf(mx, sv[u][e]);
-        if (__any(!has_ref || mx > 59.f)) {
+        const bool hides = is_tree || left < LB;
+        if (hides || __any(!has_ref || mx > 59.f)) {
+            // Hidden keys: element e of block u is key 32 u + 8 (e / 4) + e % 4 + 4 half of the tile. (Masks by
+            // arithmetic: as comparisons they would take two scalar registers each.)
+            if (hides) {
+                const unsigned long long keys = is_tree ? way : (1ull << left) - 1;
+                mx = EN_NEG_INF;
+#pragma unroll
+                for (int u = 0; u < NUW; ++u) {
+                    const uint32_t sees = (uint32_t)(keys >> (KB * (u0 + u))) >> (4 * half);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t on = (uint32_t)((int32_t)(sees << (31 - (8 * (e / 4) + e % 4))) >> 31);
+                        sv[u][e] = __uint_as_float((__float_as_uint(sv[u][e]) & on) | (0xff800000u & ~on));
+                        mx = fmaxf(mx, sv[u][e]);
+                    }
+                }
+            }
+            // a reference for rows that have none or whose scores have outgrown it
             mx = pair_max(mx);
             const bool fix = (!has_ref || mx > 59.f) && mx > EN_NEG_INF;
             const float delta = fix ? mx : 0.f;
@@ -329,29 +395,27 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     sv[u][e] -= delta;
+            probabilities(0);
         }
-        // ---- probabilities; the sums use the rounded ones, like the products ----
-        bf16x8 pf[NUW][2];
+        auto sums = [&](auto hides_tag) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < NUW; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const pair_t pb = {(bf16_t)fast_exp2(sv[u][e]), (bf16_t)fast_exp2(sv[u][e + 1])};
-                pf[u][e / 8][e % 8] = pb[0];
-                pf[u][e / 8][e % 8 + 1] = pb[1];
-                l = __builtin_amdgcn_fdot2_f32_bf16(pb, pair_t{(bf16_t)1.f, (bf16_t)1.f}, l, false);
+            for (int u = 0; u < NUW; ++u) {
+                if (u + 1 < NUW)
+                    probabilities(u + 1);
+                values(hides_tag, u);
             }
-        // ---- O^T += V^T P^T ----
+        };
+        if (hides && !is_tree)
+            sums(std::true_type{});
+        else
+            sums(std::false_type{});
+        // (the sums use the rounded probabilities, like the products)
 #pragma unroll
         for (int u = 0; u < NUW; ++u)
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int d = 0; d < NDB; ++d) {
-                    const bf16x8 v = *reinterpret_cast<const bf16x8 *>(stg + KBYTES + (32 * d + col) * VROWB +
-                                                                       ((4 * (u0 + u) + 2 * kk + half) ^ vpat) * 16);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[u][kk], o[d], 0, 0, 0);
-                }
+            for (int e = 0; e < 16; e += 2)
+                l = __builtin_amdgcn_fdot2_f32_bf16(pair_t{pf[u][e / 8][e % 8], pf[u][e / 8][e % 8 + 1]}, pair_t{(bf16_t)1.f, (bf16_t)1.f}, l,
+                                                    false);
     }
 
     l += xor32(l);
@@ -375,11 +439,12 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
         if (kw == 1)
             return;
         const f32x4 other = so[NDB * 4 * 64 + lane];
-        // (a sum is 0 where the wave had no key that the row sees, by the bits: one of NaN is not)
+        // (a sum is 0, by the bits, where the wave had no key that the row sees: one of NaN is not. The sums of values are 0
+        // then, too.)
         const bool mine = __float_as_uint(l) != 0u, its = __float_as_uint(other[1]) != 0u;
         const float m = mine && its ? fmaxf(m_ref, other[0]) : mine ? m_ref : other[0];
         const float wm = mine ? fast_exp2(m_ref - m) : 0.f, wo = its ? fast_exp2(other[0] - m) : 0.f;
-        l = (mine ? l * wm : 0.f) + (its ? other[1] * wo : 0.f);
+        l = l * wm + other[1] * wo;
         m_ref = m;
 #pragma unroll
         for (int d = 0; d < NDB; ++d)
@@ -388,14 +453,14 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
                 const f32x4 x = so[(4 * d + g) * 64 + lane];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[d][4 * g + e] = (mine ? o[d][4 * g + e] * wm : 0.f) + (its ? x[e] * wo : 0.f);
+                    o[d][4 * g + e] = o[d][4 * g + e] * wm + x[e] * wo;
             }
     }
     if (!row_there)
         return;
     if (!row_valid)
         l = 0.f;
-    if (has_tree && s_no_number) {
+    if (last_split && s_no_number) {
         // what the tree's tile left out: infinite with any weight, or NaN
 #pragma unroll 1
         for (int m = 0; m < n; ++m) {
@@ -413,19 +478,20 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
         }
     }
     if (a.n_splits > 1) {
-        const size_t part = (size_t)sp * rows_all + row;
+        const size_t part = (size_t)sp * a.n_blocks + blocks_before + block;
         if (half == 0) {
             f32x2 v = {m_ref, l};
-            *reinterpret_cast<f32x2 *>(a.ws_ml + part * 2) = v;
+            *reinterpret_cast<f32x2 *>(a.ws_ml + (part * 32 + col) * 2) = v;
         }
         if (!row_valid)
             return;                              // (a sum of 0: nobody reads the rest)
-        float *op = a.ws_opart + part * D + 4 * half;
+        // as the registers lie: a kilobyte a store, where rows would be 32 bytes here and there
+        f32x4 *op = reinterpret_cast<f32x4 *>(a.ws_opart + part * (32 * D)) + lane;
 #pragma unroll
         for (int d = 0; d < NDB; ++d)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<f32x4 *>(op + 32 * d + 8 * g) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+                op[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
     } else {
         const float inv = row_valid ? 1.f / l : 0.f;
         bf16_t *op = (bf16_t *)a.out + (((size_t)b * n + i_row) * a.Hq + hq) * D + 4 * half;
@@ -443,33 +509,37 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) void tree_attn_
 }
 
 // ---------------------------------------------------------------------------
-// tree_merge: out = sum_sp 2^(m_sp - m) O_sp / sum_sp 2^(m_sp - m) l_sp. A thread takes four values of a row, neighbours the
-// row's next four, and G groups of D / 4 threads share the splits of a row and meet in LDS. A split that a row saw nothing
-// of left a sum of 0 and no values; a row without any is zero. grid: rows * G * (D / 4) threads.
+// tree_merge: out = sum_sp 2^(m_sp - m) O_sp / sum_sp 2^(m_sp - m) l_sp. What the splits left lies as their waves' registers
+// lay: per block of rows, groups of four values per lane. The four waves of a workgroup share a group's splits and meet in
+// LDS (SHARE = 4), or take a group each, where these fill the chip. A split that a row saw nothing of left a sum of 0 and no
+// values; a row without any is zero. grid: blocks * groups * SHARE / 4.
 // ---------------------------------------------------------------------------
-template <typename T, int D, int G>
+// bf16: blocks of 32 rows, a lane's row is lane % 32, group x is dimensions 8 x + 4 (lane / 32) on
+template <typename T, int D, int SHARE>
 __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
 {
-    constexpr int CH = D / 4, RPW = 256 / (CH * G);      // threads per group; rows per workgroup
-    static_assert(RPW >= 1, "a row's groups are in a workgroup");
-    __shared__ f32x4 s_acc[G > 1 ? 256 : 1];
-    __shared__ f32x2 s_ml[G > 1 ? 256 : 1];
-    const unsigned rows = (unsigned)a.B * a.Hq * a.n;
-    const int tid = threadIdx.x, ch = tid % CH, g = tid / CH % G;
-    const unsigned row = blockIdx.x * RPW + tid / (CH * G);
-    constexpr int NB = G == 1 ? 8 : 4;
+    constexpr int GROUPS = D / 8, ROWS = 32, NB = SHARE == 4 ? 4 : 8;
+    __shared__ f32x4 s_acc[SHARE == 4 ? 256 : 1];
+    __shared__ f32x2 s_ml[SHARE == 4 ? 256 : 1];
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const unsigned item = SHARE == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+    const unsigned blk = item / GROUPS;
+    const int x = item % GROUPS, first = SHARE == 4 ? wave : 0;
+    const unsigned bh = divided(blk, a.by_blocks);       // (agent, KV head)
+    const int c_row = (blk - bh * a.head_blocks) * ROWS + lane % ROWS;
+    const bool there = c_row < (int)a.by_r.n * a.n;
     float M = EN_NEG_INF, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (row < rows)
-        for (int sp0 = g; sp0 < a.n_splits; sp0 += NB * G) {
+    if (there)
+        for (int sp0 = first; sp0 < a.n_splits; sp0 += SHARE * NB) {
             f32x2 ml[NB];
             f32x4 v[NB];
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                const bool on = sp0 + j * G < a.n_splits;
-                const size_t part = (size_t)(on ? sp0 + j * G : sp0) * rows + row;
-                ml[j] = *reinterpret_cast<const f32x2 *>(a.ws_ml + part * 2);
-                v[j] = *reinterpret_cast<const f32x4 *>(a.ws_opart + part * D + 4 * ch);
+                const bool on = sp0 + SHARE * j < a.n_splits;
+                const size_t part = (size_t)(on ? sp0 + SHARE * j : sp0) * a.n_blocks + blk;
+                ml[j] = *reinterpret_cast<const f32x2 *>(a.ws_ml + (part * ROWS + lane % ROWS) * 2);
+                v[j] = reinterpret_cast<const f32x4 *>(a.ws_opart + part * (ROWS * D))[x * 64 + lane];
                 if (!on)
                     ml[j][1] = 0.f;
             }
@@ -489,46 +559,46 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
                     acc += w * v[j];
                 }
         }
-    if constexpr (G > 1) {
+    if constexpr (SHARE == 4) {
         s_acc[tid] = acc;
         s_ml[tid] = f32x2{M, l};
         __syncthreads();
-        if (g != 0)
+        if (wave != 0)
             return;
-        f32x2 ml[G];
+        f32x2 ml[4];
 #pragma unroll
-        for (int k = 0; k < G; ++k) {
-            ml[k] = s_ml[tid + k * CH];
+        for (int k = 0; k < 4; ++k) {
+            ml[k] = s_ml[lane + 64 * k];
             M = __float_as_uint(ml[k][1]) ? fmaxf(M, ml[k][0]) : M;
         }
         l = 0.f;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < G; ++k)
+        for (int k = 0; k < 4; ++k)
             if (__float_as_uint(ml[k][1])) {
                 const float w = fast_exp2(ml[k][0] - M);
                 l += w * ml[k][1];
-                acc += w * s_acc[tid + k * CH];
+                acc += w * s_acc[lane + 64 * k];
             }
     }
-    if (row >= rows)
+    if (!there)
         return;
     const float inv = __float_as_uint(l) ? 1.f / l : 0.f;
-    const unsigned bh = divided(row, a.by_n), i = row - bh * a.n;
-    const unsigned b = divided(bh, a.by_hq), hq = bh - b * a.Hq;
+    const unsigned hl = divided(c_row, a.by_n), i = c_row - hl * a.n;
+    const unsigned b = divided(bh, a.by_hkv), hq = (bh - b * a.Hkv) * a.by_r.n + hl;
     typedef T tvec __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<tvec *>((T *)a.out + (((size_t)b * a.n + i) * a.Hq + hq) * D + 4 * ch) = __builtin_convertvector(acc * inv, tvec);
+    *reinterpret_cast<tvec *>((T *)a.out + (((size_t)b * a.n + i) * a.Hq + hq) * D + 8 * x + 4 * (lane / ROWS)) =
+        __builtin_convertvector(acc * inv, tvec);
 }
 
 template <typename T, int D>
 static void launch_merge(const EnTreeArgs &a, hipStream_t st)
 {
-    const unsigned rows = (unsigned)a.B * a.Hq * a.n;
-    const auto grid = [rows](int G) { return dim3((rows + 1024 / (D * G) - 1) / (1024 / (D * G))); };
-    if (a.n_splits > 8 && rows < 2048)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 8>), grid(8), dim3(256), 0, st, a);
+    const unsigned items = a.n_blocks * (D / 8);
+    if (items < 2048)
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), dim3(items), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), grid(1), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), dim3(items / 4), dim3(256), 0, st, a);
 }
 
 template <int D>
@@ -558,7 +628,7 @@ __global__ __launch_bounds__(256) void tree_attention_kernel(EnTreeArgs a)
     const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, kvh = hq / (a.Hq / a.Hkv);
     const int done = a.done[b];
-    const EnTreeLane mine = tree_lane(a.parent + (size_t)b * a.n, a.n, tree_room(done, a.Nq));
+    const EnTreeLane mine = tree_lane(tree_parent(a.parent + (size_t)b * a.n, a.n), a.n, tree_room(done, a.Nq));
     const unsigned long long way = readlane64(mine.way, i);
     T *out = (T *)a.out + (((size_t)b * a.n + i) * a.Hq + hq) * D;
     if (way == 0) {

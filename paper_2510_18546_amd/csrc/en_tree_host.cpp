@@ -48,19 +48,22 @@ static int check_nodes(int32_t n_nodes, const char *who)
 // ---------------------------------------------------------------------------
 // attention
 // ---------------------------------------------------------------------------
-// How a step of n nodes is cut: row blocks of a workgroup, workgroups over the rows of a KV head, splits of its keys.
+// How a step of n nodes is cut: waves of a workgroup with row blocks and the blocks that there are for them, workgroups
+// over the rows of a KV head, splits of its keys.
 struct TreeCut {
-    int blocks, n_ptiles, n_splits;
+    int blocks, tile_blocks, n_ptiles, n_splits;
+    int head_blocks;               // blocks of rows of a KV head
 };
 static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
 {
-    TreeCut c{1, 1, 1};
+    TreeCut c{1, 1, 1, 1, 1};
     if (pool->d.dtype == EN_F32)
         return c;
-    const int all = (pool->r * n + EN_ROWS_PER_WAVE - 1) / EN_ROWS_PER_WAVE;
+    const int all = c.head_blocks = (pool->r * n + EN_ROWS_PER_WAVE - 1) / EN_ROWS_PER_WAVE;
     while (c.blocks < EN_TREE_BLOCKS && c.blocks < all)
         c.blocks *= 2;
     c.n_ptiles = (all + c.blocks - 1) / c.blocks;
+    c.tile_blocks = (all + c.n_ptiles - 1) / c.n_ptiles;
     const long units = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
     const int tiles = (plan->max_ctx_len + EN_KEY_TILE - 1) / EN_KEY_TILE + 1;
     const long slots = long(pool->n_cu) * (c.blocks == 8 ? 1 : 2) * 128 / pool->d.head_dim;
@@ -72,11 +75,11 @@ static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
 struct TreeWs {
     size_t opart_off, total;
 };
-static TreeWs tree_ws(const en_pool *pool, const en_plan *plan, int n, int n_splits)
+static TreeWs tree_ws(const en_pool *pool, const en_plan *plan, const TreeCut &cut)
 {
     TreeWs w{0, 0};
-    if (n_splits > 1) {
-        const size_t parts = size_t(n_splits) * plan->B * pool->d.n_q_heads * n;
+    if (cut.n_splits > 1) {
+        const size_t parts = size_t(cut.n_splits) * plan->B * pool->d.n_kv_heads * cut.head_blocks * EN_ROWS_PER_WAVE;
         w.opart_off = (parts * 2 * sizeof(float) + 255) & ~size_t(255);
         w.total = w.opart_off + parts * pool->d.head_dim * sizeof(float);
     }
@@ -87,7 +90,7 @@ extern "C" size_t en_tree_workspace_bytes(const en_pool *pool, const en_plan *pl
 {
     if (!pool || !plan || n_nodes < 1 || n_nodes > EN_TREE_MAX_NODES)
         return 0;
-    return tree_ws(pool, plan, n_nodes, tree_cut(pool, plan, n_nodes).n_splits).total;
+    return tree_ws(pool, plan, tree_cut(pool, plan, n_nodes)).total;
 }
 
 static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n_nodes, const int32_t *done_dev,
@@ -116,14 +119,14 @@ static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n
     if (size_t(plan->ctx_stride) * pool->d.head_dim * elem > 0x7fffffffu)
         return fail(EN_ERR_UNSUPPORTED, "%s: a context of more than 2^31 - 1 bytes per KV head", who);
     const TreeCut cut = tree_cut(pool, plan, n_nodes);
-    const TreeWs ws = tree_ws(pool, plan, n_nodes, cut.n_splits);
+    const TreeWs ws = tree_ws(pool, plan, cut);
     const size_t need = ws.total;
     if (need && !ws_dev)
         return fail(EN_ERR_INVALID_ARG, "%s: workspace of %zu bytes required", who, need);
     if (ws_bytes < need)
         return fail(EN_ERR_CAPACITY, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
     const size_t units = size_t(plan->B) * pool->d.n_kv_heads * cut.n_ptiles * cut.n_splits;
-    if (units > EN_GRID_MAX / 2)
+    if (units > EN_GRID_MAX / 2 || size_t(plan->B) * pool->d.n_kv_heads * cut.head_blocks > EN_GRID_MAX / 16)
         return fail(EN_ERR_UNSUPPORTED, "%s: a step of %zu workgroups", who, units);
     if ((rc = en_ready_on_device(pool, plan, stream)) != EN_OK)
         return rc;
@@ -153,7 +156,11 @@ static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n
     a.by_splits = en_divisor(unsigned(cut.n_splits));
     a.by_hkv = en_divisor(unsigned(a.Hkv));
     a.by_n = en_divisor(unsigned(n_nodes));
-    a.by_hq = en_divisor(unsigned(a.Hq));
+    a.head_blocks = unsigned(cut.head_blocks);
+    a.n_blocks = unsigned(size_t(plan->B) * pool->d.n_kv_heads * cut.head_blocks);
+    a.by_blocks = en_divisor(a.head_blocks);
+    a.by_r = en_divisor(unsigned(pool->r));
+    a.tile_blocks = cut.tile_blocks;
     a.ws_ml = need ? static_cast<float *>(ws_dev) : nullptr;
     a.ws_opart = need ? reinterpret_cast<float *>(static_cast<char *>(ws_dev) + ws.opart_off) : nullptr;
     const bool timed = en_timing_begin(pool, stream);

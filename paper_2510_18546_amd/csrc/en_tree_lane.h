@@ -12,10 +12,9 @@ struct EnTreeLane {
 // The whole wave calls. room: new tokens that the plan has left, done to N_q (nodes of depth >= room are absent).
 // Pointer doubling: after a round a lane knows twice as much of its way, so six rounds of exchanges are the longest
 // chain, and a tree of 8 nodes takes three.
-__device__ __forceinline__ EnTreeLane tree_lane(const int32_t *parent, int n, int room)
+__device__ __forceinline__ EnTreeLane tree_lane(int p, int n, int room)          // p: the parent of node `lane`
 {
     const int lane = threadIdx.x % 64;
-    const int p = lane < n ? parent[lane] : -2;
     bool whole = p >= -1 && p < lane;            // every link looked at so far is one
     int up = whole && p >= 0 ? p : lane;         // the node that the way is known down from (a root: itself)
     unsigned long long way = (1ull << lane) | (1ull << up);
@@ -29,6 +28,12 @@ __device__ __forceinline__ EnTreeLane tree_lane(const int32_t *parent, int n, in
     t.depth = (int)__popcll(way) - 1;
     t.way = whole && t.depth < room ? way : 0ull;
     return t;
+}
+
+__device__ __forceinline__ int tree_parent(const int32_t *parent, int n)
+{
+    const int lane = threadIdx.x % 64;
+    return lane < n ? parent[lane] : -2;
 }
 
 // New tokens left to an agent that has used `done` of N_q; 0 where done is no count (an idle agent).
