@@ -297,6 +297,7 @@ struct EnTreeArgs {
     int n_splits, n_ptiles;        // of an agent's key tiles; of the r * n query rows of a KV head
     unsigned n_units;              // B * Hkv * n_splits * n_ptiles
     int tile_blocks;               // blocks of 32 rows per workgroup
+    int tree_tiles;                // key tiles that the tree's own counts as when the splits are cut
     unsigned head_blocks, n_blocks;      // blocks of 32 rows of a KV head; of all
     EnDivisor by_ptiles, by_splits, by_hkv, by_n, by_r, by_blocks;
     // what the splits leave, float32: per row (reference in log2 units, sum), [n_splits, n_blocks, 32, 2], and sums of values

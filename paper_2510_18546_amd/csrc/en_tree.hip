@@ -29,6 +29,9 @@ typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bool no_number(unsigned short bf16) { return (bf16 & 0x7f80) == 0x7f80; }
 
+#ifndef EN_TREE_AHEAD
+#define EN_TREE_AHEAD 6
+#endif
 // KW = 2: two waves share a row block, a 32-key block of every tile each, and meet at the end.
 template <int D, int RW, int KW, int NST>
 __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((amdgpu_num_vgpr(256))) void tree_attn_kernel(EnTreeArgs a)
@@ -125,8 +128,10 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
     };
     const int L = Lc + done;                     // keys of the context (an idle agent's is not used)
     const int n_ctx = room > 0 ? (L + LB - 1) / LB : 0;
-    const int t_begin = divided(sp * (n_ctx + 1) + a.n_splits - 1, a.by_splits);         // split_first_tile
-    const int t_end = min((int)divided((sp + 1) * (n_ctx + 1) + a.n_splits - 1, a.by_splits), n_ctx);
+    // (split_first_tile; the tree's tile counts as tree_tiles of them)
+    const int n_all = n_ctx + a.tree_tiles;
+    const int t_begin = min((int)divided(sp * n_all + a.n_splits - 1, a.by_splits), n_ctx);
+    const int t_end = min((int)divided((sp + 1) * n_all + a.n_splits - 1, a.by_splits), n_ctx);
     const int n_it = max(t_end - t_begin, 0) + (last_split ? 1 : 0);
     if (n_it == 0 || room == 0) {                // an agent with fewer tiles than splits, or an idle one
         nothing();
@@ -160,16 +165,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
             dma16(vt + (size_t)(W * j) * v_step, voff, dst + KBYTES + W * j * 1024);
     };
     const int ctx0 = t_begin - (last_split ? 1 : 0);     // iteration it takes tile ctx0 + it of the context
-    // The first tile is asked for here, the next ones behind the cosines and sines: these are waited for first, and loads
-    // come in the order in which they were asked for.
-    const int first_ctx = last_split ? 1 : 0;
-    if (first_ctx < n_it)
-        issue(ctx0 + first_ctx, first_ctx);
-
     const EnTreeLane tree = tree_lane(my_parent, n, room);
     const unsigned long long present = __ballot(tree.present());
     if (!present) {
-        wait_all_memory();                       // (the tiles on their way to LDS)
         nothing();
         return;
     }
@@ -197,14 +195,21 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
             cs[ks] = *reinterpret_cast<const f32x8 *>(ct + 16 * ks);
             sn[ks] = *reinterpret_cast<const f32x8 *>(st + 16 * ks);
         }
-        // (here they have come; the next tiles are on their way while they are used)
+        // Here they have come, and the tiles are asked for, which come while the queries are turned. (Loads come in the order
+        // in which they were asked for, and the compiler does not see these: asked for before the cosines and sines they
+        // would be waited for with them.)
 #pragma unroll
         for (int ks = 0; ks < NKS / 2; ++ks)
             asm volatile("" : "+v"(cs[ks]), "+v"(sn[ks]));
+        if (last_split)
+            asm volatile("" : "+v"(t_cs), "+v"(t_sn));
 #pragma unroll
-        for (int it = 1; it < NST - 1; ++it)
-            if (first_ctx < it && it < n_it)
+        for (int it = 0; it < (W < 8 ? NST - 1 : 2); ++it)
+            if (it >= (last_split ? 1 : 0) && it < n_it)
                 issue(ctx0 + it, it);
+        // (two stages: the tree's tile has no other to wait for)
+        if (NST == 2 && last_split && n_it > 1)
+            issue(ctx0 + 1, 1);
         const float scale = row_valid ? a.scale_log2e : 0.f;
 #pragma unroll
         for (int ks = 0; ks < NKS / 2; ++ks)
@@ -287,135 +292,241 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
     const int kchunk = (half ^ k_pattern(col)) * 16, vchunk = (half ^ v_pattern(col)) * 16;
     const int u0 = kw * NUW;
 
-    for (int it = 0; it < n_it; ++it) {
-        const int stage = it % NST;
-        const char *stg = smem + stage * STAGE;
-        // this tile's loads have landed when at most those of the later tiles are outstanding; all of them near the end
-        if (it + NST - 2 < n_it)
-            __builtin_amdgcn_s_waitcnt((((NST - 2) * PER) & 15) | ((((NST - 2) * PER) >> 4) << 14) | 0x0f70);
-        else
-            __builtin_amdgcn_s_waitcnt(0x0f70);
-        __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the previous tile has been read, the tree's written
-        __builtin_amdgcn_s_barrier();
-        if (it + NST - 1 < n_it)
-            issue(ctx0 + it + NST - 1, (it + NST - 1) % NST);
-        lds_data_ready();
-        const bool is_tree = last_split && it == 0;
-        const int kb = (ctx0 + it) * LB;         // first key of a context tile
-        const int left = L - kb;                 // keys of a context tile from its first on
-        if (idle)
-            continue;
-        // The products' operands and results overlap like this: the first block's scores; the second block's, beside the
-        // exponentials of the first; the first block's values, beside the exponentials of the second; the second block's
-        // values. Probabilities are taken against the reference as it is: where that has to change (or keys are hidden)
-        // those of the first block are taken again.
-        f32x16 sv[NUW];
-        bf16x8 pf[NUW][2];
-        auto scores = [&](int u) __attribute__((always_inline)) {
+    // The order of N products and the reads of their operands: EN_TREE_AHEAD reads ahead. (Left to itself the compiler
+    // reads an operand and waits for it.)
+    auto feed = [](auto n_tag) __attribute__((always_inline)) {
+        constexpr int N = decltype(n_tag)::value, A = N < EN_TREE_AHEAD ? N : EN_TREE_AHEAD;
+        __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
+        static_for<N - A>([](auto) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        });
+        __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+    };
+
+    // ---- a tile in three pieces: scores, probabilities, values; iteration `it` of the workgroup's ----
+    f32x16 sv[NUW];
+    bf16x8 pf[NUW][2];
+    auto stage_of = [&](int it) { return smem + it % NST * STAGE; };
+    auto is_tree = [&](int it) { return last_split && it == 0; };
+    auto left_of = [&](int it) { return L - (ctx0 + it) * LB; };         // keys of a context tile from its first on
+    auto score_blocks = [&](const char *stg) __attribute__((always_inline)) {
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) {
+        for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+            for (int u = 0; u < NUW; ++u) {
                 const bf16x8 fr = *reinterpret_cast<const bf16x8 *>(stg + ((u0 + u) * KB + col) * ROWB + (kchunk ^ (32 * ks)));
                 sv[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, qf[ks], ks == 0 ? negm : sv[u], 0, 0, 0);
             }
-        };
-        auto probabilities = [&](int u) __attribute__((always_inline)) {
+    };
+    auto probability_block = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                pf[u][e / 8][e % 8] = (bf16_t)fast_exp2(sv[u][e]);
-        };
-        // HIDES: the tile has columns behind the context's last token. Whatever they hold has no weight, but 0 times
-        // infinity is no 0: they become zero on their way, two columns a word.
-        auto values = [&](auto hides_tag, int u) __attribute__((always_inline)) {
-            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        for (int e = 0; e < 16; ++e)
+            pf[u][e / 8][e % 8] = (bf16_t)fast_exp2(sv[u][e]);
+    };
+    // HIDES: the tile has columns behind the context's last token. Whatever they hold has no weight, but 0 times infinity
+    // is no 0: they become zero on their way, two columns a word.
+    auto value_block = [&](const char *stg, auto hides_tag, int left, int u) __attribute__((always_inline)) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                u32x4 keep;
-                if constexpr (decltype(hides_tag)::value)
+        for (int kk = 0; kk < 2; ++kk) {
+            u32x4 keep;
+            if constexpr (decltype(hides_tag)::value)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int key = KB * (u0 + u) + 16 * kk + 4 * half + 8 * (w / 2) + 2 * (w % 2);
-                        keep[w] = key + 1 < left ? ~0u : key < left ? 0xffffu : 0u;
-                    }
-#pragma unroll
-                for (int d = 0; d < NDB; ++d) {
-                    bf16x8 v = *reinterpret_cast<const bf16x8 *>(stg + KBYTES + (32 * d + col) * VROWB +
-                                                                 (vchunk ^ (16 * (4 * (u0 + u) + 2 * kk))));
-                    if constexpr (decltype(hides_tag)::value)
-                        v = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v) & keep);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[u][kk], o[d], 0, 0, 0);
+                for (int w = 0; w < 4; ++w) {
+                    const int key = KB * (u0 + u) + 16 * kk + 4 * half + 8 * (w / 2) + 2 * (w % 2);
+                    keep[w] = key + 1 < left ? ~0u : key < left ? 0xffffu : 0u;
                 }
-            }
-        };
 #pragma unroll
-        for (int u = 0; u < NUW; ++u)
-            scores(u);
-        probabilities(0);
+            for (int d = 0; d < NDB; ++d) {
+                bf16x8 v = *reinterpret_cast<const bf16x8 *>(stg + KBYTES + (32 * d + col) * VROWB + (vchunk ^ (16 * (4 * (u0 + u) + 2 * kk))));
+                if constexpr (decltype(hides_tag)::value)
+                    v = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v) & keep);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[u][kk], o[d], 0, 0, 0);
+            }
+        }
+    };
+    // Hidden keys, and a reference for rows that have none or whose scores have outgrown it. Returns whether scores have
+    // changed.
+    auto settle_scores = [&](int it) __attribute__((always_inline)) {
         float mx = sv[0][0];
 #pragma unroll
         for (int u = 0; u < NUW; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 mx = fmaxf(mx, sv[u][e]);
-        const bool hides = is_tree || left < LB;
-        if (hides || __any(!has_ref || mx > 59.f)) {
-            // Hidden keys: element e of block u is key 32 u + 8 (e / 4) + e % 4 + 4 half of the tile. (Masks by
-            // arithmetic: as comparisons they would take two scalar registers each.)
-            if (hides) {
-                const unsigned long long keys = is_tree ? way : (1ull << left) - 1;
-                mx = EN_NEG_INF;
-#pragma unroll
-                for (int u = 0; u < NUW; ++u) {
-                    const uint32_t sees = (uint32_t)(keys >> (KB * (u0 + u))) >> (4 * half);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t on = (uint32_t)((int32_t)(sees << (31 - (8 * (e / 4) + e % 4))) >> 31);
-                        sv[u][e] = __uint_as_float((__float_as_uint(sv[u][e]) & on) | (0xff800000u & ~on));
-                        mx = fmaxf(mx, sv[u][e]);
-                    }
-                }
-            }
-            // a reference for rows that have none or whose scores have outgrown it
-            mx = pair_max(mx);
-            const bool fix = (!has_ref || mx > 59.f) && mx > EN_NEG_INF;
-            const float delta = fix ? mx : 0.f;
-            const float alpha = fix ? (has_ref ? fast_exp2(-delta) : 0.f) : 1.f;
-#pragma unroll
-            for (int d = 0; d < NDB; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    o[d][e] *= alpha;
-            l *= alpha;
-            has_ref = has_ref || fix;
-            m_ref += delta;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                negm[e] = -m_ref;
-#pragma unroll
-            for (int u = 0; u < NUW; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    sv[u][e] -= delta;
-            probabilities(0);
-        }
-        auto sums = [&](auto hides_tag) __attribute__((always_inline)) {
+        const bool hides = is_tree(it) || left_of(it) < LB;
+        if (!hides && !__any(!has_ref || mx > 59.f))
+            return false;
+        if (hides) {
+            // Element e of block u is key 32 u + 8 (e / 4) + e % 4 + 4 half of the tile. (Masks by arithmetic: as comparisons
+            // they would take two scalar registers each.)
+            const unsigned long long keys = is_tree(it) ? way : (1ull << left_of(it)) - 1;
+            mx = EN_NEG_INF;
 #pragma unroll
             for (int u = 0; u < NUW; ++u) {
-                if (u + 1 < NUW)
-                    probabilities(u + 1);
-                values(hides_tag, u);
+                const uint32_t sees = (uint32_t)(keys >> (KB * (u0 + u))) >> (4 * half);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t on = (uint32_t)((int32_t)(sees << (31 - (8 * (e / 4) + e % 4))) >> 31);
+                    sv[u][e] = __uint_as_float((__float_as_uint(sv[u][e]) & on) | (0xff800000u & ~on));
+                    mx = fmaxf(mx, sv[u][e]);
+                }
             }
-        };
-        if (hides && !is_tree)
-            sums(std::true_type{});
-        else
-            sums(std::false_type{});
-        // (the sums use the rounded probabilities, like the products)
+        }
+        mx = pair_max(mx);
+        const bool fix = (!has_ref || mx > 59.f) && mx > EN_NEG_INF;
+        const float delta = fix ? mx : 0.f;
+        const float alpha = fix ? (has_ref ? fast_exp2(-delta) : 0.f) : 1.f;
+#pragma unroll
+        for (int d = 0; d < NDB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                o[d][e] *= alpha;
+        l *= alpha;
+        has_ref = has_ref || fix;
+        m_ref += delta;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            negm[e] = -m_ref;
+#pragma unroll
+        for (int u = 0; u < NUW; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                sv[u][e] -= delta;
+        return true;
+    };
+    auto add_weights = [&]() __attribute__((always_inline)) {    // (the rounded probabilities, like the products)
 #pragma unroll
         for (int u = 0; u < NUW; ++u)
 #pragma unroll
             for (int e = 0; e < 16; e += 2)
                 l = __builtin_amdgcn_fdot2_f32_bf16(pair_t{pf[u][e / 8][e % 8], pf[u][e / 8][e % 8 + 1]}, pair_t{(bf16_t)1.f, (bf16_t)1.f}, l,
                                                     false);
+    };
+
+    if constexpr (W < 8) {
+        for (int it = 0; it < n_it; ++it) {
+            // this tile's loads have landed when at most those of the later tiles are outstanding; all of them near the end
+            if (it + NST - 2 < n_it)
+                __builtin_amdgcn_s_waitcnt((((NST - 2) * PER) & 15) | ((((NST - 2) * PER) >> 4) << 14) | 0x0f70);
+            else
+                __builtin_amdgcn_s_waitcnt(0x0f70);
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the previous tile has been read, the tree's written
+            __builtin_amdgcn_s_barrier();
+            if (it + NST - 1 < n_it && !(NST == 2 && last_split && it == 0))
+                issue(ctx0 + it + NST - 1, (it + NST - 1) % NST);
+            lds_data_ready();
+            if (idle)
+                continue;
+            // The first block's exponentials are taken beside the second block's scores, against the reference as it is, and
+            // once more where that has changed; the second's beside the first block's values.
+            const char *stg = stage_of(it);
+            score_blocks(stg);
+            feed(std::integral_constant<int, NUW * NKS>{});
+            probability_block(0);
+            if (settle_scores(it))
+                probability_block(0);
+            const int left = is_tree(it) ? LB : left_of(it);
+            auto values = [&](auto hides_tag) __attribute__((always_inline)) {
+#pragma unroll
+                for (int u = 0; u < NUW; ++u) {
+                    if (u + 1 < NUW)
+                        probability_block(u + 1);
+                    value_block(stg, hides_tag, left, u);
+                }
+            };
+            if (left < LB)
+                values(std::true_type{});
+            else
+                values(std::false_type{});
+            add_weights();
+        }
+    } else {
+        // Two waves share a SIMD, and in step they would ask for its matrix core together and then for its vector ALU
+        // together: 3850 cycles a tile of 64 keys, the sum of both. So the second four waves are half a tile behind: while
+        // one half of the waves has its products (the values of a tile and the scores of the next), the other has its
+        // exponentials. A tile's values are read until one and a half tiles behind its scores: of the four stages one is
+        // being read, one still, two are on their way.
+        static_assert(W != 8 || NST == 4, "two tiles are read at a time");
+        auto half_done = [&]() __attribute__((always_inline)) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();
+            lds_data_ready();
+        };
+        auto tile_done = [&](int it) __attribute__((always_inline)) {
+            // the next tile has landed when the one behind it is all that is outstanding
+            if (it + 2 < n_it)
+                __builtin_amdgcn_s_waitcnt((PER & 15) | ((PER >> 4) << 14) | 0x0f70);
+            else
+                __builtin_amdgcn_s_waitcnt(0x0f70);
+            half_done();
+        };
+        auto ahead = [&](int it) __attribute__((always_inline)) {
+            if (it + 2 < n_it)
+                issue(ctx0 + it + 2, (it + 2) % NST);
+        };
+        auto probabilities = [&](int it) __attribute__((always_inline)) {
+            settle_scores(it);
+            probability_block(0);
+            probability_block(1);
+            add_weights();
+        };
+        auto values = [&](int it, auto hides_tag) __attribute__((always_inline)) {
+            value_block(stage_of(it), hides_tag, left_of(it), 0);
+            value_block(stage_of(it), hides_tag, left_of(it), 1);
+        };
+        auto last_values = [&]() __attribute__((always_inline)) {
+            if (!is_tree(n_it - 1) && left_of(n_it - 1) < LB)
+                values(n_it - 1, std::true_type{});
+            else
+                values(n_it - 1, std::false_type{});
+        };
+        tile_done(-1);
+        if (idle) {
+            for (int it = 0; it < n_it; ++it) {
+                ahead(it);
+                half_done();
+                tile_done(it);
+            }
+            half_done();
+        } else if (wave < 4) {
+            for (int it = 0; it < n_it; ++it) {
+                ahead(it);
+                if (it > 0) {
+                    values(it - 1, std::false_type{});
+                    score_blocks(stage_of(it));
+                    feed(std::integral_constant<int, 2 * (NKS + 2 * NDB)>{});
+                } else {
+                    score_blocks(stage_of(it));
+                    feed(std::integral_constant<int, 2 * NKS>{});
+                }
+                half_done();
+                probabilities(it);
+                tile_done(it);
+            }
+            last_values();
+            half_done();
+        } else {
+            for (int it = 0; it < n_it; ++it) {
+                ahead(it);
+                if (it > 0)
+                    probabilities(it - 1);
+                half_done();
+                if (it > 0) {
+                    values(it - 1, std::false_type{});
+                    score_blocks(stage_of(it));
+                    feed(std::integral_constant<int, 2 * (NKS + 2 * NDB)>{});
+                } else {
+                    score_blocks(stage_of(it));
+                    feed(std::integral_constant<int, 2 * NKS>{});
+                }
+                tile_done(it);
+            }
+            probabilities(n_it - 1);
+            half_done();
+            last_values();
+        }
     }
 
     l += xor32(l);
@@ -522,7 +633,11 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
     __shared__ f32x4 s_acc[SHARE == 4 ? 256 : 1];
     __shared__ f32x2 s_ml[SHARE == 4 ? 256 : 1];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const unsigned item = SHARE == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+    // an XCD takes a run of them, as it took one of the units that left them: part of that is in its L2 still
+    const unsigned wg = (blockIdx.x % EN_XCDS) * (gridDim.x / EN_XCDS) + blockIdx.x / EN_XCDS;
+    const unsigned item = SHARE == 4 ? wg : wg * 4 + wave;
+    if (item >= a.n_blocks * GROUPS)
+        return;
     const unsigned blk = item / GROUPS;
     const int x = item % GROUPS, first = SHARE == 4 ? wave : 0;
     const unsigned bh = divided(blk, a.by_blocks);       // (agent, KV head)
@@ -596,9 +711,9 @@ static void launch_merge(const EnTreeArgs &a, hipStream_t st)
 {
     const unsigned items = a.n_blocks * (D / 8);
     if (items < 2048)
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), dim3(items), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), dim3((items + EN_XCDS - 1) / EN_XCDS * EN_XCDS), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), dim3(items / 4), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((tree_merge_kernel<T, D, 1>), dim3((items / 4 + EN_XCDS - 1) / EN_XCDS * EN_XCDS), dim3(256), 0, st, a);
 }
 
 template <int D>

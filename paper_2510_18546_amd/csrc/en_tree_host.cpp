@@ -5,7 +5,6 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 
 #include "en_internal.h"
 
@@ -53,10 +52,11 @@ static int check_nodes(int32_t n_nodes, const char *who)
 struct TreeCut {
     int blocks, tile_blocks, n_ptiles, n_splits;
     int head_blocks;               // blocks of rows of a KV head
+    int tree_tiles;                // key tiles that the tree's own counts as
 };
 static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
 {
-    TreeCut c{1, 1, 1, 1, 1};
+    TreeCut c{1, 1, 1, 1, 1, 1};
     if (pool->d.dtype == EN_F32)
         return c;
     const int all = c.head_blocks = (pool->r * n + EN_ROWS_PER_WAVE - 1) / EN_ROWS_PER_WAVE;
@@ -64,12 +64,11 @@ static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
         c.blocks *= 2;
     c.n_ptiles = (all + c.blocks - 1) / c.blocks;
     c.tile_blocks = (all + c.n_ptiles - 1) / c.n_ptiles;
+    c.tree_tiles = c.blocks == EN_TREE_BLOCKS ? 2 : 1;
     const long units = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
     const int tiles = (plan->max_ctx_len + EN_KEY_TILE - 1) / EN_KEY_TILE + 1;
     const long slots = long(pool->n_cu) * (c.blocks == 8 ? 1 : 2) * 128 / pool->d.head_dim;
     c.n_splits = int(std::max<long>(1, std::min<long>(std::min<long>(slots / std::max<long>(1, units), tiles), EN_MAX_SPLITS)));
-    if (const char *e = getenv("EN_TREE_SPLITS"))
-        c.n_splits = std::min(std::min(atoi(e), tiles), 64);
     return c;
 }
 struct TreeWs {
@@ -161,6 +160,7 @@ static int segmented_tree_attention_impl(en_pool *pool, en_plan *plan, int32_t n
     a.by_blocks = en_divisor(a.head_blocks);
     a.by_r = en_divisor(unsigned(pool->r));
     a.tile_blocks = cut.tile_blocks;
+    a.tree_tiles = cut.tree_tiles;
     a.ws_ml = need ? static_cast<float *>(ws_dev) : nullptr;
     a.ws_opart = need ? reinterpret_cast<float *>(static_cast<char *>(ws_dev) + ws.opart_off) : nullptr;
     const bool timed = en_timing_begin(pool, stream);
@@ -276,9 +276,7 @@ static int check_logits(int32_t vocab, int32_t dtype, const void *p, int64_t str
 // Rows of an agent that a workgroup takes.
 static int rules_nodes(const EnRulesArgs &a)
 {
-    long want = (a.rules.penalties_dev ? 4 : 16) * 256;
-    if (const char *e = getenv("EN_RN"))
-        want = atoi(e) * 256;
+    const long want = (a.rules.penalties_dev ? 2 : 1) * 256;
     const long groups = std::min<long>(a.n, std::max<long>(1, want / (long(a.B) * a.chunks)));
     return int((a.n + groups - 1) / groups);
 }

@@ -10,18 +10,20 @@ struct EnTreeLane {
 };
 
 // The whole wave calls. room: new tokens that the plan has left, done to N_q (nodes of depth >= room are absent).
-// Pointer doubling: after a round a lane knows twice as much of its way, so six rounds of exchanges are the longest
-// chain, and a tree of 8 nodes takes three.
+// Pointer doubling: after a round a lane knows twice as much of its way, so seven rounds of exchanges see the longest chain to
+// its end, and a tree of depth 6 takes four.
 __device__ __forceinline__ EnTreeLane tree_lane(int p, int n, int room)          // p: the parent of node `lane`
 {
     const int lane = threadIdx.x % 64;
     bool whole = p >= -1 && p < lane;            // every link looked at so far is one
     int up = whole && p >= 0 ? p : lane;         // the node that the way is known down from (a root: itself)
-    unsigned long long way = (1ull << lane) | (1ull << up);
-    for (int known = 1; known < n; known *= 2) {
-        way |= __shfl(way, up, 64);
+    unsigned long long way = (1ull << lane) | (1ull << up);      // .. with all nodes on the way there
+    while (true) {
         const int next = __shfl(up | (whole ? 0 : 64), up, 64);
         whole = whole && next < 64;
+        if (!__any((next & 63) != up))           // all ways are known up to their ends
+            break;
+        way |= __shfl(way, up, 64);
         up = next & 63;
     }
     EnTreeLane t;
