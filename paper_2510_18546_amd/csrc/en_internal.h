@@ -311,6 +311,7 @@ struct EnTreeCommitArgs {
     const float *cos_tab, *sin_tab;
     const int32_t *hdr, *done, *accepted, *path;
     int B, Hkv, Nq, n, T, layers;
+    EnDivisor by_hkv;
     const void *k_rows[EN_TREE_COMMIT_LAYERS], *v_rows[EN_TREE_COMMIT_LAYERS];
     void *kc[EN_TREE_COMMIT_LAYERS], *vt[EN_TREE_COMMIT_LAYERS];
 };

@@ -733,94 +733,268 @@ static int launch_tree_bf16(const EnTreeArgs &a, int blocks, hipStream_t st)
     return (int)hipGetLastError();
 }
 // ---------------------------------------------------------------------------
-// tree_attention: one workgroup per (agent, query head, node), 256 keys at a time: a thread takes the score of a key,
-// the workgroup their maximum and sum, then a thread one dimension of a part of the keys.
+// tree_f32: the same in single precision on the fp32 matrix instruction (16 x 16 x 4), for small layers, which are bound by
+// latency. As in attn_f32_kernel a workgroup takes 16 rows of a KV head, its eight waves share a split's keys 16 at a time
+// and meet in LDS; no operand goes through LDS. The blocks of the tree's own keys follow those of the context: a lane holds
+// both halves of the pairs of its key, so it turns them in its registers.
 // ---------------------------------------------------------------------------
-template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_attention_kernel(EnTreeArgs a)
+template <int D>
+__global__ __launch_bounds__(512) void tree_f32_kernel(EnTreeArgs a)
 {
-    __shared__ float sq[D], sp[256], sred[4], sacc[256];
-    const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z;
-    const int tid = threadIdx.x, kvh = hq / (a.Hq / a.Hkv);
-    const int done = a.done[b];
-    const EnTreeLane mine = tree_lane(tree_parent(a.parent + (size_t)b * a.n, a.n), a.n, tree_room(done, a.Nq));
-    const unsigned long long way = readlane64(mine.way, i);
-    T *out = (T *)a.out + (((size_t)b * a.n + i) * a.Hq + hq) * D;
-    if (way == 0) {
-        if (tid < D)
-            out[tid] = (T)0.f;
-        return;
-    }
-    const int L = a.hdr[4 * b + 1] + done;
-    const int pos = L + __builtin_amdgcn_readlane(mine.depth, i);
-    if (tid < D / 2) {
-        const T *q = (const T *)a.q + (((size_t)b * a.n + i) * a.Hq + hq) * D;
-        const float c = a.cos_tab[(size_t)pos * (D / 2) + tid], s = a.sin_tab[(size_t)pos * (D / 2) + tid];
-        rope_scale_pair((float)q[tid], (float)q[tid + D / 2], c, s, a.scale_log2e, sq[tid], sq[tid + D / 2]);
-    }
-    __syncthreads();
-    const size_t slab = (size_t)b * a.Hkv + kvh;
-    float m = EN_NEG_INF, l = 0.f, acc = 0.f;
-    const int d = tid % D, part = tid / D;
-    constexpr int PARTS = 256 / D;
-    for (int k0 = 0; k0 < L + 64; k0 += 256) {
-        // keys 0 .. L - 1: the context; L .. L + 63: the nodes
-        const int key = k0 + tid, node = key - L;
-        float s = EN_NEG_INF;
-        if (node < 0) {
-            const T *k = (const T *)a.kc + (slab * a.T + key) * D;
-            s = 0.f;
-            for (int c = 0; c < D; ++c)
-                s += sq[c] * (float)k[c];
-        } else if (node < 64 && (way >> node & 1)) {
-            const T *k = (const T *)a.k_rows + (((size_t)b * a.n + node) * a.Hkv + kvh) * D;
-            const size_t p = L + __popcll(way & ((1ull << node) - 1));
-            s = 0.f;
-            for (int c = 0; c < D / 2; ++c) {
-                float y1, y2;
-                rope_key_pair((float)k[c], (float)k[c + D / 2], a.cos_tab[p * (D / 2) + c], a.sin_tab[p * (D / 2) + c], y1, y2);
-                s += sq[c] * (float)(T)y1 + sq[c + D / 2] * (float)(T)y2;
-            }
-        }
-        float mx = wave_max(s);
-        __syncthreads();
-        if (tid % 64 == 0)
-            sred[tid / 64] = mx;
-        __syncthreads();
-        mx = fmaxf(fmaxf(sred[0], sred[1]), fmaxf(sred[2], sred[3]));
-        const float now = fmaxf(m, mx), ref = now == EN_NEG_INF ? 0.f : now, keep = fast_exp2(m - ref);
-        m = now;
-        const float p = s == EN_NEG_INF ? 0.f : fast_exp2(s - ref);
-        sp[tid] = p;
-        const float ps = wave_sum(p);
-        __syncthreads();
-        if (tid % 64 == 0)
-            sred[tid / 64] = ps;
-        __syncthreads();
-        l = l * keep + ((sred[0] + sred[1]) + (sred[2] + sred[3]));
-        acc *= keep;
-        for (int j = part; j < 256; j += PARTS) {
-            const int kj = k0 + j, nj = kj - L;
-            if (nj < 0) {
-                float v;
-                if constexpr (sizeof(T) == 4)
-                    v = ((const float *)a.vt)[(slab * a.T + kj) * D + d];
-                else
-                    v = (float)((const T *)a.vt)[(slab * D + d) * a.T + ((kj & ~0xC) | ((kj & 4) << 1) | ((kj & 8) >> 1))];
-                acc += sp[j] * v;
-            } else if (nj < 64 && (way >> nj & 1)) {
-                acc += sp[j] * (float)((const T *)a.v_rows)[(((size_t)b * a.n + nj) * a.Hkv + kvh) * D + d];
-            }
-        }
-    }
-    sacc[tid] = acc;
-    __syncthreads();
-    if (tid < D) {
-        float sum = 0.f;
+    constexpr int WAVES = 8, ROWS = EN_F32_ROWS, KEYS = 16;
+    constexpr int NJ = D / 16;                   // 16-byte loads per key row and lane; blocks of O^T
+    constexpr int NV = D / 64;                   // 16-byte loads per value row and lane
+    constexpr int OSTR = D + 4;                  // floats per merged row in LDS
+    __shared__ __attribute__((aligned(16))) float so[WAVES][ROWS][OSTR];
+    __shared__ f32x2 sml[WAVES][ROWS];           // (reference, sum) of a wave's rows
+
+    // (arguments and divisions: see attn_bf16_kernel)
+    asm volatile("" ::"s"(a.q), "s"(a.k_rows), "s"(a.kc), "s"(a.vt), "s"(a.cos_tab), "s"(a.hdr), "s"(a.parent), "s"(a.B), "s"(a.n),
+                 "s"(a.by_ptiles.mul), "s"(a.by_splits.mul), "s"(a.by_hkv.mul), "s"(a.by_n.mul), "s"(a.by_r.n), "s"(a.ws_ml));
+    const unsigned t = divided(blockIdx.x, a.by_ptiles);
+    const int rg = blockIdx.x - t * a.n_ptiles;
+    const unsigned t2 = divided(t, a.by_splits);
+    const int sp = t - t2 * a.n_splits;
+    const int b = divided(t2, a.by_hkv);
+    const int kvh = t2 - b * a.Hkv;
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int lane = tid % 64;
+    const int col = lane % 16, grp = lane / 16;
+    const int r = a.by_r.n, n = a.n;
+
+    const int done = as_table(a.done)[b];
+    const int Lc = as_table(a.hdr)[4 * b + 1];
+    const int my_parent = tree_parent(a.parent + (size_t)b * n, n);
+    const int n_rows = r * n;
+    const int r0 = rg * ROWS, r1 = min(r0 + ROWS, n_rows) - 1;
+    const int rr = min(r0 + col, r1);
+    const int hl = divided(rr, a.by_n), i_row = rr - hl * n;
+    f32x4 qf[NJ];
+    {
+        const float *qp = (const float *)a.q + (((size_t)b * n + i_row) * a.Hq + kvh * r + hl) * D + 4 * grp;
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p)
-            sum += sacc[p * D + tid];
-        out[tid] = (T)(sum / l);
+        for (int j = 0; j < NJ; ++j)
+            qf[j] = *reinterpret_cast<const f32x4 *>(qp + 16 * j);
+    }
+    const int room = tree_room(done, a.Nq);
+    const int L = Lc + done;                     // keys of the context (an idle agent's is not used)
+    const int n_ctx = room > 0 ? (L + KEYS - 1) / KEYS : 0, n_blk = room > 0 ? n_ctx + (n + KEYS - 1) / KEYS : 0;
+    const int first = divided(sp * n_blk + a.n_splits - 1, a.by_splits), last = divided((sp + 1) * n_blk + a.n_splits - 1, a.by_splits);
+    const int per = (last - first + WAVES - 1) / WAVES;
+    const int wb = min(first + wave * per, last), we = min(first + (wave + 1) * per, last);      // this wave's blocks
+    const float *const K = (const float *)a.kc + ((size_t)b * a.Hkv + kvh) * (size_t)a.T * D;
+    const float *const V = (const float *)a.vt + ((size_t)b * a.Hkv + kvh) * (size_t)a.T * D;
+    const size_t own = ((size_t)b * n * a.Hkv + kvh) * D;
+    const float *const Kt = (const float *)a.k_rows + own, *const Vt = (const float *)a.v_rows + own;
+    // (context rows reach up to a multiple of 64 keys: whole blocks can be read)
+    f32x4 kf[NJ], vf[4][NV];
+    auto load_block = [&](int blk) {
+        const bool tree = blk >= n_ctx;
+        const int k0 = (blk - (tree ? n_ctx : 0)) * KEYS;
+        const float *const kb = tree ? Kt : K, *const vb = tree ? Vt : V;
+        const size_t stride = tree ? (size_t)a.Hkv * D : D;
+        const int most = tree ? n - 1 : 0x7fffffff;
+        const float *kr = kb + min(k0 + col, most) * stride + 4 * grp;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            kf[j] = *reinterpret_cast<const f32x4 *>(kr + 16 * j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float *vr = vb + min(k0 + 4 * grp + e, most) * stride + col * NJ;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                vf[e][v] = *reinterpret_cast<const f32x4 *>(vr + 4 * v);
+        }
+    };
+    if (wb < we)
+        load_block(wb);
+
+    const EnTreeLane tree = tree_lane(my_parent, n, room);
+    const unsigned long long row_way = __shfl(tree.way, i_row, 64);      // (all lanes exchange)
+    const unsigned long long way = r0 + col <= r1 ? row_way : 0ull;
+    const bool row_valid = way != 0;
+    // ---- the query, rotated at its node's position and scaled ----
+    {
+        const int depth = __shfl(tree.depth, i_row, 64);
+        const size_t at = (size_t)(room > 0 ? L + (row_valid ? depth : 0) : 0) * (D / 2) + 4 * grp;
+#pragma unroll
+        for (int j = 0; j < NJ / 2; ++j) {
+            const f32x4 cs = *reinterpret_cast<const f32x4 *>(a.cos_tab + at + 16 * j);
+            const f32x4 sn = *reinterpret_cast<const f32x4 *>(a.sin_tab + at + 16 * j);
+            const f32x4 x1 = qf[j], x2 = qf[j + NJ / 2];
+            qf[j] = (x1 * cs - x2 * sn) * a.scale_log2e;
+            qf[j + NJ / 2] = (x2 * cs + x1 * sn) * a.scale_log2e;
+        }
+        if (!row_valid)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                qf[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    f32x4 o[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+        o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = EN_NEG_INF, l = 0.f;                       // l: this lane's share
+    auto row_sum = [](float v) {                         // over the four lanes of a row
+        v += __shfl_xor(v, 16, 64);
+        return v + xor32(v);
+    };
+    for (int blk = wb; blk < we; ++blk) {
+        const bool of_tree = blk >= n_ctx;
+        const int k0 = (blk - (of_tree ? n_ctx : 0)) * KEYS;
+        if (of_tree) {
+            const int node = min(k0 + col, n - 1);
+            const int depth = __popcll(__shfl(tree.way, node, 64)) - 1;
+            const size_t at = (size_t)(L + max(depth, 0)) * (D / 2) + 4 * grp;
+#pragma unroll
+            for (int j = 0; j < NJ / 2; ++j) {
+                const f32x4 cs = *reinterpret_cast<const f32x4 *>(a.cos_tab + at + 16 * j);
+                const f32x4 sn = *reinterpret_cast<const f32x4 *>(a.sin_tab + at + 16 * j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y1, y2;
+                    rope_key_pair(kf[j][e], kf[j + NJ / 2][e], cs[e], sn[e], y1, y2);
+                    kf[j][e] = y1;
+                    kf[j + NJ / 2][e] = y2;
+                }
+            }
+        }
+        // ---- scores; eight chains of products, whose sums meet in a tree (see attn_f32_kernel) ----
+        f32x4 s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int i = (e * NJ + j) % 8;
+                s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][e], qf[j][e], s[i], 0, 0, 0);
+            }
+        // the lane's keys are 4 grp + e of the block
+        const uint32_t sees = of_tree ? (uint32_t)(way >> k0) >> (4 * grp) : L - k0 >= KEYS ? 0xfu : ((1u << (L - k0)) - 1u) >> (4 * grp);
+        const uint32_t there = of_tree ? 0xfu : sees;
+        f32x4 vc[4][NV];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)      // (what lies behind the context's last token counts as zero)
+                    vc[e][v][x] = __uint_as_float(there >> e & 1 ? __float_as_uint(vf[e][v][x]) : 0u);
+        if (blk + 1 < we)
+            load_block(blk + 1);
+        f32x4 p = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(sees >> e & 1))
+                p[e] = EN_NEG_INF;
+        float mn = fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3]));
+        mn = fmaxf(mn, __shfl_xor(mn, 16, 64));
+        mn = fmaxf(m, pair_max(mn));
+        const float ref = mn == EN_NEG_INF ? 0.f : mn;   // nothing seen yet: all exponentials are 0
+        const float alpha = fast_exp2(m - ref);
+        m = mn;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            p[e] = fast_exp2(p[e] - ref);
+        l = l * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
+        // ---- O^T += V^T P^T (the block's products by themselves: one rounding per block of a sum that grows). A hidden
+        // key's value that is infinite or NaN has no place in a product with 0: then the keys go one by one, and a row
+        // keeps its sums where it does not see the key. ----
+        f32x4 ob[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            ob[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        bool by_key = false;
+        if (of_tree) {
+            uint32_t top = 0;                            // (by the bits: this library is built without NaN compares)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    top = max(top, __float_as_uint(vc[e][j / 4][j % 4]) & 0x7f800000u);
+            by_key = __any(top == 0x7f800000u);
+        }
+        if (!by_key) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    ob[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vc[e][j / 4][j % 4], p[e], ob[j], 0, 0, 0);
+        } else {
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const f32x4 with = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            grp == g ? vc[e][j / 4][j % 4] : 0.f, grp == g ? p[e] : 0.f, ob[j], 0, 0, 0);
+                        ob[j] = way >> (k0 + 4 * g + e) & 1 ? with : ob[j];
+                    }
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            o[j] = o[j] * alpha + ob[j];
+    }
+
+    // ---- the waves meet ----
+    {
+        const float lt = row_sum(l);
+        if (grp == 0)
+            sml[wave][col] = f32x2{m, row_valid ? lt : 0.f};     // (a sum of 0: no key that the row sees)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                f32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[j] = o[4 * v + j][e];
+                *reinterpret_cast<f32x4 *>(&so[wave][col][(4 * grp + e) * NJ + 4 * v]) = x;
+            }
+    }
+    __syncthreads();
+    // ---- the output, a 16-byte piece per thread at a time ----
+    constexpr int CPR = D / 4;
+    static_assert(ROWS * CPR % 256 == 0, "whole waves");
+    for (int x = tid; x < ROWS * CPR; x += 64 * WAVES) {
+        const int row = x / CPR, c4 = x % CPR * 4, c_row = r0 + row;
+        if (c_row > r1)
+            break;
+        float M = EN_NEG_INF, sum = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        f32x2 ml[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            ml[w] = sml[w][row];
+            M = __float_as_uint(ml[w][1]) ? fmaxf(M, ml[w][0]) : M;
+        }
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const f32x4 part = *reinterpret_cast<const f32x4 *>(&so[w][row][c4]);
+            if (__float_as_uint(ml[w][1])) {
+                const float wt = fast_exp2(ml[w][0] - M);
+                sum += ml[w][1] * wt;
+                acc += part * wt;
+            }
+        }
+        if (a.n_splits > 1) {
+            // as tree_merge_kernel reads it
+            const size_t part = (size_t)sp * a.n_blocks + ((unsigned)b * a.Hkv + kvh) * a.head_blocks + c_row / 32;
+            if (c4 == 0) {
+                f32x2 v = {M, sum};
+                *reinterpret_cast<f32x2 *>(a.ws_ml + (part * 32 + c_row % 32) * 2) = v;
+            }
+            reinterpret_cast<f32x4 *>(a.ws_opart + part * (32 * D))[c4 / 8 * 64 + c_row % 32 + c4 / 4 % 2 * 32] = acc;
+        } else {
+            const int ho = divided(c_row, a.by_n), i = c_row - ho * n;
+            const float inv = __float_as_uint(sum) ? 1.f / sum : 0.f;
+            *reinterpret_cast<f32x4 *>((float *)a.out + (((size_t)b * n + i) * a.Hq + kvh * r + ho) * D + c4) = acc * inv;
+        }
     }
 }
 
@@ -830,11 +1004,11 @@ int en_launch_tree_attention(const en_pool *pool, const EnTreeArgs &a, int block
     const int D = pool->d.head_dim;
     if (pool->d.dtype != EN_F32)
         return D == 64 ? launch_tree_bf16<64>(a, blocks, st) : launch_tree_bf16<128>(a, blocks, st);
-    const dim3 grid(a.n, a.Hq, a.B), blk(256);
+    const dim3 grid(a.n_units), blk(512);
     if (D == 64)
-        hipLaunchKernelGGL((tree_attention_kernel<float, 64>), grid, blk, 0, st, a);
+        hipLaunchKernelGGL((tree_f32_kernel<64>), grid, blk, 0, st, a);
     else
-        hipLaunchKernelGGL((tree_attention_kernel<float, 128>), grid, blk, 0, st, a);
+        hipLaunchKernelGGL((tree_f32_kernel<128>), grid, blk, 0, st, a);
     return (int)hipGetLastError();
 }
 
@@ -856,35 +1030,79 @@ int en_launch_tree_merge(const en_pool *pool, const EnTreeArgs &a, void *stream)
 }
 
 // ---------------------------------------------------------------------------
-// tree_commit: entry j of an agent's path goes to context row L_c + (done - accepted) + j, the key rotated there. grid:
-// (n, Hkv * layers, B), D/2 threads: thread c owns the rotary pair (c, c + D/2).
+// tree_commit: entry j of an agent's path goes to context row L_c + (done - accepted) + j, the key rotated there. A workgroup
+// takes a KV head of a layer and agent, all of its tokens: four tokens at positions 4 x to 4 x + 3 are eight bytes side by
+// side in a row of the transposed values, and a store of two bytes costs the memory as much as one of eight. Bound by those
+// rows: D lines per (layer, agent, KV head), read and written back whatever the tokens are. grid: (Hkv * layers, B).
 // ---------------------------------------------------------------------------
 template <typename T, int D>
-__global__ __launch_bounds__(D / 2) void tree_commit_kernel(EnTreeCommitArgs a)
+__global__ __launch_bounds__(D) void tree_commit_kernel(EnTreeCommitArgs a)
 {
-    const int j = blockIdx.x, layer = blockIdx.y / a.Hkv, h = blockIdx.y - layer * a.Hkv, b = blockIdx.z;
-    const int c = threadIdx.x;
-    const int accepted = a.accepted[b], row = a.done[b] - accepted + j;
-    const int node = a.path[(size_t)b * a.n + j];
-    if (j >= accepted || (unsigned)node >= (unsigned)a.n || (unsigned)row >= (unsigned)a.Nq)
+    constexpr int HALF = D / 2;
+    const int b = blockIdx.y, layer = divided(blockIdx.x, a.by_hkv), h = blockIdx.x - layer * a.Hkv;
+    const int tid = threadIdx.x, lane = tid % 64;
+    const int most = min(as_table(a.accepted)[b], a.n);
+    const int row0 = (int)((unsigned)as_table(a.done)[b] - (unsigned)as_table(a.accepted)[b]);       // of the plan's new tokens
+    const int Lc = as_table(a.hdr)[4 * b + 1];
+    const int my_node = lane < most ? a.path[(size_t)b * a.n + lane] : -1;
+    // entries that are a node and have a place
+    const unsigned long long valid = __ballot((unsigned)my_node < (unsigned)a.n && row0 + lane >= 0 && row0 + lane < a.Nq && row0 >= -64);
+    if (valid == 0)
         return;
-    const size_t pos = (size_t)a.hdr[4 * b + 1] + row;
-    const size_t from = (((size_t)b * a.n + node) * a.Hkv + h) * D, slab = (size_t)b * a.Hkv + h;
-    const T *kr = (const T *)a.k_rows[layer] + from, *vr = (const T *)a.v_rows[layer] + from;
-    float y1, y2;
-    rope_key_pair((float)kr[c], (float)kr[c + D / 2], a.cos_tab[pos * (D / 2) + c], a.sin_tab[pos * (D / 2) + c], y1, y2);
-    T *kd = (T *)a.kc[layer] + (slab * a.T + pos) * D;
-    kd[c] = (T)y1;
-    kd[c + D / 2] = (T)y2;
+    const size_t slab = (size_t)b * a.Hkv + h;
+    const size_t step = (size_t)a.Hkv * D, from = (size_t)b * a.n * step + h * D;
+    const T *const kr = (const T *)a.k_rows[layer] + from, *const vr = (const T *)a.v_rows[layer] + from;
+    T *const kd = (T *)a.kc[layer] + slab * a.T * D, *const vd = (T *)a.vt[layer] + slab * a.T * D;
+    const int pos0 = Lc + row0;
+    auto node_of = [&](int j) { return __builtin_amdgcn_readlane(my_node, j); };
+    // keys, two tokens at a time: thread c and c + D/2 own the pair (c, c + D/2) of one each
+    const int c = tid % HALF, second = tid / HALF;
+    for (unsigned long long todo = valid; todo;) {
+        const int j1 = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int j2 = todo ? __builtin_ctzll(todo) : j1;
+        todo &= todo - 1;
+        const int j = second ? j2 : j1, node = second ? node_of(j2) : node_of(j1);
+        const size_t pos = (size_t)(pos0 + j);
+        float y1, y2;
+        rope_key_pair((float)kr[node * step + c], (float)kr[node * step + c + HALF], a.cos_tab[pos * HALF + c], a.sin_tab[pos * HALF + c], y1, y2);
+        kd[pos * D + c] = (T)y1;
+        kd[pos * D + c + HALF] = (T)y2;
+    }
     if constexpr (sizeof(T) == 4) {
-        T *vd = (T *)a.vt[layer] + (slab * a.T + pos) * D;
-        vd[c] = vr[c];
-        vd[c + D / 2] = vr[c + D / 2];
+        for (unsigned long long todo = valid; todo; todo &= todo - 1) {
+            const int j = __builtin_ctzll(todo);
+            vd[(size_t)(pos0 + j) * D + tid] = vr[node_of(j) * step + tid];
+        }
     } else {
-        // transposed layout [D][T], token j in column j with bits 2 and 3 exchanged
-        T *vd = (T *)a.vt[layer] + slab * D * a.T + ((pos & ~(size_t)0xC) | ((pos & 4) << 1) | ((pos & 8) >> 1));
-        vd[(size_t)c * a.T] = vr[c];
-        vd[(size_t)(c + D / 2) * a.T] = vr[c + D / 2];
+        // values: thread d owns row d of the transposed layout, token t in column t with bits 2 and 3 exchanged
+        typedef unsigned short u16;
+        const u16 *const v_in = (const u16 *)vr + tid;
+        u16 *const v_out = (u16 *)vd + (size_t)tid * a.T;
+        const int j_first = __builtin_ctzll(valid), j_last = 63 - __builtin_clzll(valid);
+        for (int t0 = (pos0 + j_first) & ~3; t0 <= pos0 + j_last; t0 += 4) {
+            const int j0 = t0 - pos0;                    // entry of token t0; -3 at least
+            const unsigned there = (unsigned)(j0 >= 0 ? valid >> j0 : valid << -j0) & 15u;
+            u16 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = there >> k & 1 ? v_in[node_of(j0 + k) * step] : 0;
+            u16 *const to = v_out + ((t0 & ~0xC) | ((t0 & 4) << 1) | ((t0 & 8) >> 1));
+            if (there == 15u) {
+                *reinterpret_cast<u16x4 *>(to) = u16x4{v[0], v[1], v[2], v[3]};
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k += 2) {
+                    const unsigned pair = there >> k & 3u;
+                    if (pair == 3u)
+                        *reinterpret_cast<uint32_t *>(to + k) = (uint32_t)v[k] | (uint32_t)v[k + 1] << 16;
+                    else if (pair == 1u)
+                        to[k] = v[k];
+                    else if (pair == 2u)
+                        to[k + 1] = v[k + 1];
+                }
+            }
+        }
     }
 }
 
@@ -892,7 +1110,7 @@ int en_launch_tree_commit(const en_pool *pool, const EnTreeCommitArgs &a, void *
 {
     const hipStream_t st = (hipStream_t)stream;
     const int D = pool->d.head_dim;
-    const dim3 grid(a.n, a.Hkv * a.layers, a.B), blk(D / 2);
+    const dim3 grid(a.Hkv * a.layers, a.B), blk(D);
     if (pool->d.dtype == EN_F32) {
         if (D == 64)
             hipLaunchKernelGGL((tree_commit_kernel<float, 64>), grid, blk, 0, st, a);

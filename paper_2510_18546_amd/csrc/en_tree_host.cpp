@@ -57,9 +57,25 @@ struct TreeCut {
 static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
 {
     TreeCut c{1, 1, 1, 1, 1, 1};
-    if (pool->d.dtype == EN_F32)
-        return c;
     const int all = c.head_blocks = (pool->r * n + EN_ROWS_PER_WAVE - 1) / EN_ROWS_PER_WAVE;
+    if (pool->d.dtype == EN_F32) {
+        // As choose_splits for the fp32 attention: rounds of workgroups times the 16-key blocks that a wave of them takes,
+        // and two for its start and end; splits cost the merge.
+        c.n_ptiles = (pool->r * n + EN_F32_ROWS - 1) / EN_F32_ROWS;
+        const long base = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
+        const int all_blocks = (plan->max_ctx_len + 15) / 16 + (n + 15) / 16;
+        long best_cost = -1;
+        for (int s = 1; s <= std::min((all_blocks + EN_WAVES - 1) / EN_WAVES, EN_MAX_SPLITS); ++s) {
+            const long rounds = (base * s + pool->n_cu - 1) / pool->n_cu;
+            const long blocks = ((all_blocks + s - 1) / s + EN_WAVES - 1) / EN_WAVES;
+            const long cost = rounds * (blocks + 2) + (s > 1 ? 128 / pool->d.head_dim : 0);
+            if (best_cost < 0 || cost < best_cost) {
+                best_cost = cost;
+                c.n_splits = s;
+            }
+        }
+        return c;
+    }
     while (c.blocks < EN_TREE_BLOCKS && c.blocks < all)
         c.blocks *= 2;
     c.n_ptiles = (all + c.blocks - 1) / c.blocks;
@@ -222,6 +238,7 @@ static int segmented_tree_commit_impl(en_pool *pool, en_plan *plan, int32_t n_no
     a.Nq = plan->Nq;
     a.n = n_nodes;
     a.T = plan->ctx_stride;
+    a.by_hkv = en_divisor(unsigned(a.Hkv));
     for (int l0 = 0; l0 < n_layers; l0 += EN_TREE_COMMIT_LAYERS) {
         a.layers = n_layers - l0 < EN_TREE_COMMIT_LAYERS ? n_layers - l0 : EN_TREE_COMMIT_LAYERS;
         for (int l = 0; l < a.layers; ++l) {
@@ -276,7 +293,7 @@ static int check_logits(int32_t vocab, int32_t dtype, const void *p, int64_t str
 // Rows of an agent that a workgroup takes.
 static int rules_nodes(const EnRulesArgs &a)
 {
-    const long want = (a.rules.penalties_dev ? 2 : 1) * 256;
+    const long want = (a.rules.penalties_dev ? 4 : 1) * 256;
     const long groups = std::min<long>(a.n, std::max<long>(1, want / (long(a.B) * a.chunks)));
     return int((a.n + groups - 1) / groups);
 }
