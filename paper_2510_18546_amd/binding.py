@@ -479,8 +479,8 @@ def _buffer(name: str, t, nbytes: int, dev: int) -> int:
 def _all_at(name: str, ts, nbytes: int, dtype, dev: int, exact: bool) -> array.array:
     """Addresses of the layers' tensors, contiguous, of (`exact`) or of at least that many bytes, on the device."""
     t_ = _torch().Tensor
-    sizes = list(map(t_.nbytes.__get__, ts))
-    if (min(sizes) < nbytes or exact and (max(sizes) != nbytes or any(t.dtype is not dtype for t in ts)) or
+    sizes = set(map(t_.nbytes.__get__, ts))
+    if (min(sizes) < nbytes or exact and (max(sizes) != nbytes or set(map(t_.dtype.__get__, ts)) != {dtype}) or
             not all(map(t_.is_contiguous, ts)) or set(map(t_.get_device, ts)) != {dev}):
         raise ValueError(f"{name}: a contiguous tensor of {'' if exact else 'at least '}{nbytes} bytes{f' of {dtype}' if exact else ''} on "
                          "the current device is wanted for every layer")

@@ -42,8 +42,8 @@ __device__ __forceinline__ void wave_lds_order()
 
 // ---------------------------------------------------------------------------
 // rules: a workgroup takes EN_RULES_CHUNK tokens of `a.nodes` of an agent's rows, a wave a quarter of the tokens of each
-// row: 16 a lane, in two runs of eight. Bound by reading the logits once (and writing them once); several rows' loads are
-// on their way while one is looked at, and a choice is found with few exchanges between lanes.
+// row: 16 a lane, in two runs of eight. Bound by reading the logits once (and writing them once); a choice is found with few
+// exchanges between lanes.
 //
 // The tokens that penalties concern are few: they are counted into a table in LDS once for all rows of the workgroup, each
 // wave lists those of its quarter, and in a row only they are divided and subtracted from, in a copy of the quarter in
@@ -57,17 +57,17 @@ struct EnRun {                       // eight logits as they lie in a row
     T x[8];
 } __attribute__((packed, aligned(sizeof(T))));
 
+// Of so many tokens that have occurred a wave's list is worth its trips through LDS.
+constexpr int EN_RULES_LISTED = 256;
 struct EnRulesLds {
     float x[4][EN_RULES_CHUNK / 4];
     int count[EN_RULES_CHUNK];
-    unsigned short hit[4][EN_RULES_CHUNK / 4];
+    unsigned short hit[4][EN_RULES_LISTED];
 };
-// Of so many tokens that have occurred a wave's list is worth its trips through LDS.
-constexpr int EN_RULES_LISTED = 256;
 
-// RULED: there may be penalties, a bias or a mask. DEPTH: rows on their way.
-template <typename T, bool CHOOSE, bool RULED, int DEPTH>
-__global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
+// RULED: there may be penalties, a bias or a mask.
+template <typename T, bool CHOOSE, bool RULED>
+__global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a)
 {
     constexpr int WAVE_TOKENS = EN_RULES_CHUNK / 4;      // 1024
     static_assert(WAVE_TOKENS == 1024, "two runs of eight a lane");
@@ -118,16 +118,10 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
     struct Row {
         EnRun<T> run[2];
         uint32_t allowed[2];
-        int node;                                        // -1: none
-    } ring[DEPTH];
-    unsigned long long todo = last > 0 ? rows : 0ull;
-    auto load = [&](Row &x) __attribute__((always_inline)) {
-        x.node = todo ? __builtin_ctzll(todo) : -1;
-        if (!todo)
-            return;
-        todo &= todo - 1;
-        const T *row = (const T *)a.logits + ((size_t)b * a.n + x.node) * a.logits_stride + w0;
-        const uint32_t *words = RULED && mask ? mask + (size_t)x.node * r.mask_node_stride : nullptr;
+    };
+    auto load = [&](int i, Row &x) __attribute__((always_inline)) {
+        const T *row = (const T *)a.logits + ((size_t)b * a.n + i) * a.logits_stride + w0;
+        const uint32_t *words = RULED && mask ? mask + (size_t)i * r.mask_node_stride : nullptr;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int k = 512 * q + 8 * lane;
@@ -142,9 +136,10 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
                 x.allowed[q] = k < last ? words[(w0 + k) >> 5] : 0u;
         }
     };
-#pragma unroll
-    for (int k = 0; k < DEPTH; ++k)
-        load(ring[k]);
+    unsigned long long todo = last > 0 ? rows : 0ull;
+    Row now;
+    if (todo)
+        load(__builtin_ctzll(todo), now);
 
     const float *const bias = RULED && r.bias_dev ? r.bias_dev + (size_t)b * r.bias_agent_stride : nullptr;
     float add[2][8];
@@ -199,8 +194,9 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const unsigned long long hits = __ballot(c[k] > 0);
-            if (c[k] > 0)
-                lds.hit[wave][n_hit + __popcll(hits & ((1ull << lane) - 1))] = (unsigned short)(64 * k + lane);
+            const int at = n_hit + (int)__popcll(hits & ((1ull << lane) - 1));
+            if (c[k] > 0 && at < EN_RULES_LISTED)        // (a longer list is not used)
+                lds.hit[wave][at] = (unsigned short)(64 * k + lane);
             n_hit += (int)__popcll(hits);
         }
         wave_lds_order();
@@ -260,8 +256,7 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
             atomicSub(&count[my_token], 1);
         wave_lds_order();
     };
-    auto look_at = [&](const Row &in) __attribute__((always_inline)) {
-        const int i = in.node;
+    auto look_at = [&](int i, const Row &in) __attribute__((always_inline)) {
         float x[2][8];
 #pragma unroll
         for (int q = 0; q < 2; ++q)
@@ -331,13 +326,14 @@ __global__ __launch_bounds__(256) void rules_kernel(EnRulesArgs a)
             }
         }
     };
-    while (ring[0].node >= 0)
-        static_for<DEPTH>([&](auto k) {
-            if (ring[k].node >= 0) {
-                look_at(ring[k]);
-                load(ring[k]);
-            }
-        });
+    // (One row at a time: many waves with few registers hide the memory's latency better than a wave with several rows on
+    // their way. Choices of 64 x 32 rows of 128000 tokens, bf16: one row 91 us, two 93, three 120, four 116, eight 151.)
+    while (todo) {
+        look_at(__builtin_ctzll(todo), now);
+        todo &= todo - 1;
+        if (todo)
+            load(__builtin_ctzll(todo), now);
+    }
 
     if constexpr (CHOOSE) {
         const int waves = min(4, (a.vocab - v0 + WAVE_TOKENS - 1) / WAVE_TOKENS);    // those that had tokens
@@ -406,24 +402,24 @@ __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
     }
 }
 
-template <typename T, bool CHOOSE, int DEPTH>
+template <typename T, bool CHOOSE>
 static int launch_rules(const EnRulesArgs &a, hipStream_t st)
 {
     const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks), blk(256);
     const size_t lds = a.rules.penalties_dev ? sizeof(EnRulesLds) : 0;
     if (a.rules.penalties_dev || a.rules.bias_dev || a.rules.mask_dev)
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true, 2>), grid, blk, lds, st, a);
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true>), grid, blk, lds, st, a);
     else
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false, DEPTH>), grid, blk, 0, st, a);
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false>), grid, blk, 0, st, a);
     return (int)hipGetLastError();
 }
 int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream)
 {
-    return dtype == EN_F32 ? launch_rules<float, false, 2>(a, (hipStream_t)stream) : launch_rules<bf16_t, false, 4>(a, (hipStream_t)stream);
+    return dtype == EN_F32 ? launch_rules<float, false>(a, (hipStream_t)stream) : launch_rules<bf16_t, false>(a, (hipStream_t)stream);
 }
 int en_launch_choices(const EnRulesArgs &a, int dtype, void *stream)
 {
-    return dtype == EN_F32 ? launch_rules<float, true, 2>(a, (hipStream_t)stream) : launch_rules<bf16_t, true, 4>(a, (hipStream_t)stream);
+    return dtype == EN_F32 ? launch_rules<float, true>(a, (hipStream_t)stream) : launch_rules<bf16_t, true>(a, (hipStream_t)stream);
 }
 
 int en_launch_accept(const EnAcceptArgs &a, void *stream)
