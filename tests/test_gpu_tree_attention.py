@@ -75,10 +75,10 @@ def test_absent_nodes_idle_agents_and_the_reserve(dtype):
 
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [9, 40])
-def test_rows_that_are_no_numbers_reach_their_descendants_only(dtype, value, n):
+@pytest.mark.parametrize("n,r,d", [(9, 3, 64), (40, 3, 64), (64, 7, 128), (30, 2, 128)])
+def test_rows_that_are_no_numbers_reach_their_descendants_only(dtype, value, n, r, d):
     """A drafted token's rows of NaN or infinity: nodes beside it are what they are without it."""
-    t = Tree(n, dtype, [130, 50], [1, 0], 70, [comb(n), comb(n)], r=3, kv=1)
+    t = Tree(n, dtype, [130, 50], [1, 0], 70, [comb(n), comb(n)], r=r, kv=1, d=d)
     want = t.expected()
     t.k[0][0, 4, 0, 5] = value
     t.v[0][1, 5, 0, ::3] = value
@@ -101,12 +101,10 @@ def test_rows_that_are_no_numbers_reach_their_descendants_only(dtype, value, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_context_rows_behind_the_last_token_are_not_looked_at(dtype):
-    a = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=np.nan)
-    b = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=np.inf)
-    c = Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, 9), fill=0.0)
+@pytest.mark.parametrize("n,r,d", [(9, 2, 64), (16, 4, 128), (64, 7, 128), (64, 4, 64)])
+def test_context_rows_behind_the_last_token_are_not_looked_at(dtype, n, r, d):
     import torch
-    outs = [t.attend() for t in (a, b, c)]
+    outs = [Tree(5, dtype, [97, 64, 0], [3, 0, 1], 70, forest(3, n), r=r, d=d, fill=fill).attend() for fill in (np.nan, np.inf, 0.0)]
     torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
@@ -128,6 +126,38 @@ def test_large_scores(dtype):
     else:
         # a rounded query's score is off by 64 * 0.02 (see near): weights by factors, outputs stay within the values
         assert np.abs(got).max() <= np.abs(t.values[0][np.isfinite(t.values[0])]).max() + np.abs(t.v).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,r,d", [(4, 2, 64), (13, 4, 128), (32, 4, 128), (64, 8, 128), (64, 4, 64)])
+@pytest.mark.parametrize("direction", [1, -1])
+def test_scores_that_grow_or_fall_along_the_context(dtype, n, r, d, direction):
+    """Along the context the keys turn from pointing away from every query to pointing at it, scores from -100 to 100 in steps
+    of two per 64 keys, or the other way round: references have to follow, by factors far beyond what an exponent holds.
+    The direction that the scores come from is one that no position turns (the last pair's angle is below 0.02 here)."""
+    length = 6400
+    t = Tree(2, dtype, [length, 320], [0, 3], 80, forest(2, n, ("comb", "chain")), r=r, kv=1, d=d)
+    u = np.zeros(d, np.float32)
+    u[d // 2 - 1] = 1.0
+    ramp = (np.arange(t.T, dtype=np.float32) / length * 2 - 1) * 100 * direction
+    t.q[:] = 0.25 * t.q + np.sqrt(d) * u / 2
+    t.keys[:] = 0.25 * t.keys + ramp[:, None] * u * 2
+    t.k[:] = 0.25 * t.k
+    if dtype == "bf16":
+        from tree_cases import bf16
+        t.q, t.keys, t.k = bf16(t.q), bf16(t.keys), bf16(t.k)
+    t.up()
+    t.kc = [t.device(x) for x in t.keys]
+    import torch
+    got = t.attend()
+    torch.cuda.synchronize()
+    got, want = got.float().cpu().numpy(), t.expected()
+    assert np.isfinite(got).all()
+    # a score of 100 is known to 100 * 2^-24 * a few roundings in fp32, to 100 * 2^-8 / sqrt(3) of the one product that makes it
+    # in bf16 (the query is rounded, by the same factor for all keys): neighbours in weight differ by steps of 2 / 64 a key,
+    # so that weights over some 30 keys are off by a tenth at most
+    err = np.abs(got - want)
+    assert (err <= (2e-4 if t.f32 else 0.25) * np.maximum(1.0, np.abs(want))).all(), err.max()
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
@@ -201,6 +231,29 @@ def test_captured_and_replayed(dtype):
         assert np.array_equal(got, eager.float().cpu().numpy())
         t.done, t.parent = done, parent
         near(got, t.expected(), t.f32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_calls_at_once(dtype):
+    """Two streams, two scratch buffers, one plan: the calls only read what they share."""
+    import torch
+    t = Tree(3, dtype, [3000, 900], [3, 8], 60, forest(2, 33), r=4, kv=2, d=64)
+    want = t.attend()
+    torch.cuda.synchronize()
+    streams, outs, scratch = [torch.cuda.Stream() for _ in range(2)], [], [t.ws, t.ws.clone()]
+    for _ in range(4):
+        for s, ws in zip(streams, scratch):
+            t.ws = ws
+            with torch.cuda.stream(s):
+                outs.append(t.attend())
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in outs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,n_new", [(64, 5), (64, 1), (10, 10)])
+def test_more_nodes_than_the_reserve(dtype, n, n_new):
+    check(Tree(n, dtype, [77, 5, 64], [0, n_new - 1, n_new // 2], n_new, forest(3, n, ("star", "comb", "chain"))))
 
 
 def test_timed_like_the_other_attention_calls():
