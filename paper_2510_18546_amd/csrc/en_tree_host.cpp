@@ -83,7 +83,13 @@ static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
     c.tree_tiles = c.blocks == EN_TREE_BLOCKS ? 2 : 1;
     const long units = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
     const int tiles = (plan->max_ctx_len + EN_KEY_TILE - 1) / EN_KEY_TILE + 1;
-    const long slots = long(pool->n_cu) * (c.blocks == 8 ? 1 : 2) * 128 / pool->d.head_dim;
+    // Workgroups: one to a compute unit; two where each would have more than twelve tiles, which then hide each other's starts
+    // and ends (a workgroup of eight blocks has a compute unit to itself). Attention and merge, us, one / two to a compute
+    // unit: 1 agent of 8 KV heads x 4 K tokens, 8 nodes 15.2 / 17.2, 16 nodes 16.3 / 20.0, x 12 K, 4 nodes 18.8 / 19.6, 4
+    // agents x 4 K, 32 nodes 28.9 / 33.6, 2 x 3 K, 16 nodes of 64 values 13.4 / 14.6; 16 agents x 2 K (15 tiles), 13 nodes 37.1 /
+    // 35.7, x 8 K (63), 8 nodes 126.8 / 124.3.
+    const long all_tiles = units * tiles;
+    const long slots = long(pool->n_cu) * (c.blocks < EN_TREE_BLOCKS && all_tiles > 12L * pool->n_cu ? 2 : 1);
     c.n_splits = int(std::max<long>(1, std::min<long>(std::min<long>(slots / std::max<long>(1, units), tiles), EN_MAX_SPLITS)));
     return c;
 }
