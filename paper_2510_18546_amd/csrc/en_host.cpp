@@ -11,6 +11,7 @@
 #include <memory>
 #include <new>
 #include <string>
+#include <thread>
 
 #include "en_internal.h"
 
@@ -236,12 +237,36 @@ static int pool_ensure_device(en_pool *p)
     std::vector<double> theta(half);
     for (int k = 0; k < half; ++k)
         theta[k] = std::pow(p->d.rope_base, -2.0 * double(k) / double(p->d.head_dim));
-    for (int pos = 0; pos < p->d.max_ctx; ++pos)
-        for (int k = 0; k < half; ++k) {
-            const double a = double(pos) * theta[k];
-            c[size_t(pos) * half + k] = float(std::cos(a));
-            s[size_t(pos) * half + k] = float(std::sin(a));
+    const auto rows = [&](int from, int to) {
+        for (int pos = from; pos < to; ++pos)
+            for (int k = 0; k < half; ++k) {
+                const double a = double(pos) * theta[k];
+                c[size_t(pos) * half + k] = float(std::cos(a));
+                s[size_t(pos) * half + k] = float(std::sin(a));
+            }
+    };
+    {
+        // A first call waits for this: long tables by up to eight threads (8.7 K positions of 64 pairs: 20 ms by one).
+        struct Team {
+            std::vector<std::thread> threads;
+            ~Team()
+            {
+                for (std::thread &t : threads)
+                    t.join();
+            }
+        } team;
+        const int most = int(std::min<unsigned>(8, std::max(1u, std::thread::hardware_concurrency())));
+        const int parts = std::max(1, std::min(most, int(n / 16384)));
+        const auto bound = [&](int i) { return int(int64_t(p->d.max_ctx) * i / parts); };
+        int shared = 0;                            // parts that threads have taken
+        try {
+            for (team.threads.reserve(parts); shared + 1 < parts; ++shared)
+                team.threads.emplace_back(rows, bound(shared), bound(shared + 1));
+        } catch (const std::exception &) {
+            // (no more threads: the rest is done here)
         }
+        rows(bound(shared), p->d.max_ctx);
+    }
     hipError_t e;
     if ((e = hipMalloc((void **)&p->d_cos, n * sizeof(float))) != hipSuccess)
         return hip_fail(e, "hipMalloc(rotary table)");
