@@ -41,14 +41,16 @@ __device__ __forceinline__ void wave_lds_order()
 }
 
 // ---------------------------------------------------------------------------
-// rules: a workgroup takes EN_RULES_CHUNK tokens of `a.nodes` of an agent's rows, a wave a quarter of the tokens of each
-// row: 16 a lane, in two runs of eight. Bound by reading the logits once (and writing them once); a choice is found with few
-// exchanges between lanes.
+// rules: a workgroup takes EN_RULES_CHUNK tokens of `a.nodes` of an agent's rows, a wave an equal share of the tokens of each
+// row: 16 a lane, in two runs of eight, or one run. Reading the logits once (and writing them once) is all that choices
+// without rules cost: 64 x 32 rows of 128000 tokens, bf16, 91 us, 5.8 TB/s; one agent's eight rows of 32000 3.8, which is a
+// launch and two trips to memory. Under penalties the tables' set-up comes first (7 us with 2 - 4 K tokens of history), then
+// the instructions a token: all rules on 16 x 13 rows of 50021 tokens 18.2 us, choices of 128000 under all rules 25.8.
 //
 // The tokens that penalties concern are few: they are counted into a table in LDS once for all rows of the workgroup, each
-// wave lists those of its quarter, and in a row only they are divided and subtracted from, in a copy of the quarter in
+// wave lists those of its share, and in a row only they are divided and subtracted from, in a copy of the share in
 // LDS (a division for every token would be 12 of 40 instructions a token, and these instructions more time than the
-// logits' way from memory). Tokens of a node's own way join the counts for that row; mostly none lies in the quarter.
+// logits' way from memory). Tokens of a node's own way join the counts for that row; mostly none lies in the share.
 // Rows need not be aligned: loads of 16 bytes from any element on. grid: (groups of nodes, B, chunks): the first tokens, which
 // in most vocabularies are the frequent ones, are begun first.
 // ---------------------------------------------------------------------------
@@ -57,23 +59,28 @@ struct EnRun {                       // eight logits as they lie in a row
     T x[8];
 } __attribute__((packed, aligned(sizeof(T))));
 
-// Of so many tokens that have occurred a wave's list is worth its trips through LDS.
-constexpr int EN_RULES_LISTED = 256;
 struct EnRulesLds {
-    float x[4][EN_RULES_CHUNK / 4];
+    float x[EN_RULES_CHUNK];
     int count[EN_RULES_CHUNK];
-    unsigned short hit[4][EN_RULES_LISTED];
+    unsigned short hit[EN_RULES_CHUNK / 4];
 };
+
+// Rules that are written out take eight waves with half as many tokens each: 16 agents' 13 rows of 50021 tokens 19.1 us with
+// four, 18.2 with eight, one row of 32000 6.1 / 5.2. Choices have a wave's exchanges for each row besides: 16 x 13 rows of
+// 128000 tokens under all rules 25.8 / 27.2.
+constexpr int en_rules_waves(bool choose, bool ruled) { return ruled && !choose ? 8 : 4; }
 
 // RULED: there may be penalties, a bias or a mask.
 template <typename T, bool CHOOSE, bool RULED>
-__global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a)
+__global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rules_waves(CHOOSE, RULED) : 1) void rules_kernel(EnRulesArgs a)
 {
-    constexpr int WAVE_TOKENS = EN_RULES_CHUNK / 4;      // 1024
-    static_assert(WAVE_TOKENS == 1024, "two runs of eight a lane");
+    constexpr int WAVES = en_rules_waves(CHOOSE, RULED), NT = 64 * WAVES;
+    constexpr int WAVE_TOKENS = EN_RULES_CHUNK / WAVES;
+    constexpr int Q = WAVE_TOKENS / 512;                 // runs of eight a lane
+    constexpr int LISTED = WAVE_TOKENS / 4;              // of so many tokens that have occurred a list is worth its trips through LDS
     extern __shared__ __attribute__((aligned(16))) char smem[];      // EnRulesLds, if there are penalties
     EnRulesLds &lds = *reinterpret_cast<EnRulesLds *>(smem);
-    __shared__ unsigned long long s_best[CHOOSE ? EN_TREE_MAX_NODES : 1][4];
+    __shared__ unsigned long long s_best[CHOOSE ? EN_TREE_MAX_NODES : 1][WAVES];
     const int chunk = blockIdx.z, b = blockIdx.y, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
     const int i0 = blockIdx.x * a.nodes, i1 = min(i0 + a.nodes, a.n);
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         const int most = history ? r.history_stride : 0;
 #pragma unroll
         for (int j = 0; j < HJ; ++j)
-            early[j] = j * 256 + tid < most ? history[j * 256 + tid] : -1;
+            early[j] = j * NT + tid < most ? history[j * NT + tid] : -1;
         if (a.tokens && lane < a.n)
             token = a.tokens[(size_t)b * a.n + lane];
         rep = r.penalties_dev[3 * b];
@@ -116,14 +123,14 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
 
     // a lane's run q: tokens w0 + 512 q + 8 lane on
     struct Row {
-        EnRun<T> run[2];
-        uint32_t allowed[2];
+        EnRun<T> run[Q];
+        uint32_t allowed[Q];
     };
     auto load = [&](int i, Row &x) __attribute__((always_inline)) {
         const T *row = (const T *)a.logits + ((size_t)b * a.n + i) * a.logits_stride + w0;
         const uint32_t *words = RULED && mask ? mask + (size_t)i * r.mask_node_stride : nullptr;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < Q; ++q) {
             const int k = 512 * q + 8 * lane;
             if (k + 8 <= last)
                 x.run[q] = *reinterpret_cast<const EnRun<T> *>(row + k);
@@ -142,10 +149,10 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         load(__builtin_ctzll(todo), now);
 
     const float *const bias = RULED && r.bias_dev ? r.bias_dev + (size_t)b * r.bias_agent_stride : nullptr;
-    float add[2][8];
+    float add[Q][8];
     if (RULED && bias)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < Q; ++q) {
             const int k = 512 * q + 8 * lane;
             EnRun<float> run;
             if (k + 8 <= last)
@@ -158,13 +165,14 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
             for (int j = 0; j < 8; ++j)
                 add[q][j] = run.x[j];
         }
-    int n_hit = 0, my_token = -1;                        // my_token: of node `lane`, in the quarter, or -1
+    int n_hit = 0, my_token = -1;                        // my_token: of node `lane`, in the share, or -1
     int *const count = lds.count + wave * WAVE_TOKENS;
+    unsigned short *const hit = lds.hit + wave * LISTED;
     if (penalties_on) {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int k = 0; k < EN_RULES_CHUNK / 1024; ++k)
-            *reinterpret_cast<i32x4 *>(lds.count + 1024 * k + 4 * tid) = i32x4{0, 0, 0, 0};
+        for (int k = 0; k < EN_RULES_CHUNK / (4 * NT); ++k)
+            *reinterpret_cast<i32x4 *>(lds.count + 4 * NT * k + 4 * tid) = i32x4{0, 0, 0, 0};
         {
             const unsigned v = (unsigned)token - (unsigned)w0;
             my_token = tree.present() && token >= 0 && v < (unsigned)max(last, 0) ? (int)v : -1;
@@ -176,35 +184,35 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         };
 #pragma unroll
         for (int j = 0; j < HJ; ++j)
-            counted(early[j], j * 256 + tid < h);
-        for (int k0 = HJ * 256; k0 < h; k0 += HJ * 256) {
+            counted(early[j], j * NT + tid < h);
+        for (int k0 = HJ * NT; k0 < h; k0 += HJ * NT) {
             int v[HJ];
 #pragma unroll
             for (int j = 0; j < HJ; ++j)
-                v[j] = k0 + j * 256 + tid < h ? history[k0 + j * 256 + tid] : -1;
+                v[j] = k0 + j * NT + tid < h ? history[k0 + j * NT + tid] : -1;
 #pragma unroll
             for (int j = 0; j < HJ; ++j)
-                counted(v[j], k0 + j * 256 + tid < h);
+                counted(v[j], k0 + j * NT + tid < h);
         }
         __syncthreads();
-        int c[16];
+        int c[8 * Q];
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
+        for (int k = 0; k < 8 * Q; ++k)
             c[k] = 64 * k + lane < last ? count[64 * k + lane] : 0;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
+        for (int k = 0; k < 8 * Q; ++k) {
             const unsigned long long hits = __ballot(c[k] > 0);
             const int at = n_hit + (int)__popcll(hits & ((1ull << lane) - 1));
-            if (c[k] > 0 && at < EN_RULES_LISTED)        // (a longer list is not used)
-                lds.hit[wave][at] = (unsigned short)(64 * k + lane);
+            if (c[k] > 0 && at < LISTED)                 // (a longer list is not used)
+                hit[at] = (unsigned short)(64 * k + lane);
             n_hit += (int)__popcll(hits);
         }
         wave_lds_order();
     }
-    const unsigned long long in_quarter = RULED ? __ballot(my_token >= 0) : 0ull;
+    const unsigned long long in_share = RULED ? __ballot(my_token >= 0) : 0ull;
 
-    auto penalties = [&](float (&x)[2][8], unsigned long long way) __attribute__((always_inline)) {
-        const bool own = (way & in_quarter) != 0;
+    auto penalties = [&](float (&x)[Q][8], unsigned long long way) __attribute__((always_inline)) {
+        const bool own = (way & in_share) != 0;
         if (n_hit == 0 && !own)
             return;
         const bool adds = own && my_token >= 0 && (way >> lane & 1);
@@ -212,10 +220,10 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         if (adds)
             first = atomicAdd(&count[my_token], 1) == 0;
         wave_lds_order();
-        if (n_hit > EN_RULES_LISTED) {
+        if (n_hit > LISTED) {
             // so many that every lane looks at its own tokens
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int q = 0; q < Q; ++q)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4) {
                     typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -227,22 +235,22 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
                     }
                 }
         } else {
-            float *const sx = lds.x[wave];
+            float *const sx = lds.x + wave * WAVE_TOKENS;
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int q = 0; q < Q; ++q)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4)
                     *reinterpret_cast<f32x4 *>(sx + 512 * q + 8 * lane + j) = f32x4{x[q][j], x[q][j + 1], x[q][j + 2], x[q][j + 3]};
             wave_lds_order();
             for (int k = lane; k < n_hit; k += 64) {
-                const int t = lds.hit[wave][k];
+                const int t = hit[k];
                 sx[t] = penalised(sx[t], count[t], rep, freq, pres);
             }
             if (first)
                 sx[my_token] = penalised(sx[my_token], count[my_token], rep, freq, pres);
             wave_lds_order();
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int q = 0; q < Q; ++q)
 #pragma unroll
                 for (int j = 0; j < 8; j += 4) {
                     const f32x4 y = *reinterpret_cast<const f32x4 *>(sx + 512 * q + 8 * lane + j);
@@ -257,9 +265,9 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         wave_lds_order();
     };
     auto look_at = [&](int i, const Row &in) __attribute__((always_inline)) {
-        float x[2][8];
+        float x[Q][8];
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 x[q][j] = (float)in.run[q].x[j];
@@ -268,13 +276,13 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
                 penalties(x, a.parent ? readlane64(tree.way, i) : 0ull);
             if (bias)
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < Q; ++q)
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         x[q][j] += add[q][j];
             if (mask)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < Q; ++q) {
                     const uint32_t bits = in.allowed[q] >> (8 * lane & 31);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -284,23 +292,23 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         if constexpr (CHOOSE) {
             // The largest of each run, of the wave, the first lane that has it in its first run or else in its second, and
             // which of the run's it is: of equals the lowest token. (NaN is no maximum.)
-            float top_of[2];
+            float top_of[Q];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int q = 0; q < Q; ++q) {
                 top_of[q] = EN_NEG_INF;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     top_of[q] = fmaxf(top_of[q], x[q][j]);
             }
-            const float top = wave_max(fmaxf(top_of[0], top_of[1]));
-            const unsigned long long in0 = __ballot(top_of[0] == top), in1 = __ballot(top_of[1] == top);
+            const float top = wave_max(fmaxf(top_of[0], top_of[Q - 1]));
+            const unsigned long long in0 = __ballot(top_of[0] == top), in1 = __ballot(top_of[Q - 1] == top);
             unsigned long long w = 0;
             if (top > EN_NEG_INF) {
                 const int l = __builtin_ctzll(in0 ? in0 : in1);
                 int at = 7;
 #pragma unroll
                 for (int j = 6; j >= 0; --j) {
-                    const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(in0 ? x[0][j] : x[1][j]), l));
+                    const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(in0 ? x[0][j] : x[Q - 1][j]), l));
                     at = y == top ? j : at;
                 }
                 w = (unsigned long long)rank_of(top) << 32 | (unsigned)~(w0 + (in0 ? 0 : 512) + 8 * l + at);
@@ -310,7 +318,7 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
         } else {
             T *row = (T *)a.out + ((size_t)b * a.n + i) * a.out_stride + w0;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int q = 0; q < Q; ++q) {
                 const int k = 512 * q + 8 * lane;
                 EnRun<T> run;
 #pragma unroll
@@ -336,7 +344,7 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
     }
 
     if constexpr (CHOOSE) {
-        const int waves = min(4, (a.vocab - v0 + WAVE_TOKENS - 1) / WAVE_TOKENS);    // those that had tokens
+        const int waves = min(WAVES, (a.vocab - v0 + WAVE_TOKENS - 1) / WAVE_TOKENS);    // those that had tokens
         __syncthreads();
         const int row = i0 + tid;
         if (row < i1 && (rows >> row & 1)) {
@@ -348,7 +356,8 @@ __global__ __launch_bounds__(256, RULED ? 4 : 1) void rules_kernel(EnRulesArgs a
     }
 }
 
-// A workgroup per agent: the choices out of their chunks' best, a wave a node, then the first wave goes down the path.
+// accept: a workgroup per agent: the choices out of their chunks' best, a wave a node, then the first wave goes down the path,
+// a ballot a node. Bound by latency: 8 nodes with 8 chunks each 2.6 us, 64 agents' 32 nodes with 32 chunks 5.0.
 __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
 {
     __shared__ int s_choice[EN_TREE_MAX_NODES];
@@ -405,12 +414,12 @@ __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
 template <typename T, bool CHOOSE>
 static int launch_rules(const EnRulesArgs &a, hipStream_t st)
 {
-    const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks), blk(256);
+    const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks);
     const size_t lds = a.rules.penalties_dev ? sizeof(EnRulesLds) : 0;
     if (a.rules.penalties_dev || a.rules.bias_dev || a.rules.mask_dev)
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true>), grid, blk, lds, st, a);
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true>), grid, dim3(64 * en_rules_waves(CHOOSE, true)), lds, st, a);
     else
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false>), grid, blk, 0, st, a);
+        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false>), grid, dim3(64 * en_rules_waves(CHOOSE, false)), 0, st, a);
     return (int)hipGetLastError();
 }
 int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream)
