@@ -408,7 +408,8 @@ int segmented_decode_step_static(en_pool *pool, en_plan *plan, int32_t q_first, 
  *   out_dev                : device, [B, n_nodes, Hq, D]; rows of absent nodes
  *                            are set to zero
  *   ws_dev, ws_bytes       : scratch of at least en_tree_workspace_bytes, 16-byte
- *                            aligned, or NULL where that is 0
+ *                            aligned, or NULL where that is 0; calls that overlap
+ *                            have scratch of their own (so has token_tree_accept)
  * Arrays of rows and contexts are 16-byte aligned. What absent nodes' rows
  * hold, or nodes outside a way, makes no difference, infinities and NaN
  * included.
@@ -468,7 +469,8 @@ typedef struct en_token_rules {
  *                     by parent_dev alone here.)
  * Errors: INVALID_ARG (null, non-positive sizes, strides below vocab,
  *         alignment to an element), UNSUPPORTED (dtype, n_nodes >
- *         EN_TREE_MAX_NODES), DEVICE.
+ *         EN_TREE_MAX_NODES, more than 65535 agents or 65535 * 4096 tokens),
+ *         DEVICE.
  */
 int token_rules_apply(const en_token_rules *rules, int32_t n_agents, int32_t n_nodes, int32_t vocab, int32_t dtype,
                       const int32_t *parent_dev, const int32_t *tokens_dev, const void *logits_dev,
@@ -517,8 +519,8 @@ int token_tree_accept(const en_plan *plan, const en_token_rules *rules, int32_t 
  * node, and rows outside the plan's reserve, are left out; no other row is
  * written.
  * Errors: INVALID_ARG (null, n_layers < 0, n_nodes < 1, alignment), UNSUPPORTED
- *         (n_nodes > EN_TREE_MAX_NODES, a plan whose values stay in the pool),
- *         DEVICE.
+ *         (n_nodes > EN_TREE_MAX_NODES, a plan whose values stay in the pool,
+ *         more than 65535 agents), DEVICE.
  */
 #define EN_TREE_COMMIT_LAYERS 64
 int segmented_tree_commit(en_pool *pool, en_plan *plan, int32_t n_nodes, int32_t n_layers, const int32_t *done_dev,

@@ -222,6 +222,8 @@ static int segmented_tree_commit_impl(en_pool *pool, en_plan *plan, int32_t n_no
         return rc;
     if (!aligned(done_dev, 4) || !aligned(n_accepted_dev, 4) || !aligned(path_dev, 4))
         return fail(EN_ERR_INVALID_ARG, "%s: int32 arrays must be 4-byte aligned", who);
+    if (plan->B > EN_GRID_YZ_MAX)
+        return fail(EN_ERR_UNSUPPORTED, "%s: more than %d agents", who, EN_GRID_YZ_MAX);
     for (int l = 0; l < n_layers; ++l) {
         if (!k_rows_dev[l] || !v_rows_dev[l] || !kc_dev[l] || !vt_dev[l])
             return fail(EN_ERR_INVALID_ARG, "%s: null pointer for layer %d", who, l);
@@ -304,6 +306,12 @@ static int rules_nodes(const EnRulesArgs &a)
     const long groups = std::min<long>(a.n, std::max<long>(1, 4 * 256 / (long(a.B) * a.chunks)));
     return int((a.n + groups - 1) / groups);
 }
+static int check_grid(int32_t n_agents, int32_t chunks, const char *who)
+{
+    if (n_agents > EN_GRID_YZ_MAX || chunks > EN_GRID_YZ_MAX)
+        return fail(EN_ERR_UNSUPPORTED, "%s: more than %d agents or %lld tokens", who, EN_GRID_YZ_MAX, (long long)EN_GRID_YZ_MAX * EN_RULES_CHUNK);
+    return EN_OK;
+}
 static int chunks_of(int32_t vocab) { return int((int64_t(vocab) + EN_RULES_CHUNK - 1) / EN_RULES_CHUNK); }
 
 static int token_rules_apply_impl(const en_token_rules *rules, int32_t n_agents, int32_t n_nodes, int32_t vocab,
@@ -317,6 +325,8 @@ static int token_rules_apply_impl(const en_token_rules *rules, int32_t n_agents,
     int rc;
     if ((rc = check_nodes(n_nodes, who)) != EN_OK || (rc = check_logits(vocab, dtype, logits_dev, logits_stride, who)) != EN_OK ||
         (rc = check_logits(vocab, dtype, out_dev, out_stride, who)) != EN_OK || (rc = check_rules(*rules, vocab, who)) != EN_OK)
+        return rc;
+    if ((rc = check_grid(n_agents, chunks_of(vocab), who)) != EN_OK)
         return rc;
     if (out_dev == logits_dev && out_stride != logits_stride)
         return fail(EN_ERR_INVALID_ARG, "%s: in place with another stride", who);
@@ -368,6 +378,8 @@ static int token_tree_accept_impl(const en_plan *plan, const en_token_rules *rul
     int rc = check_nodes(n_nodes, who);
     if (rc != EN_OK)
         return rc;
+    if ((rc = check_grid(plan->B, 0, who)) != EN_OK)
+        return rc;
     for (const void *p : {(const void *)done_dev, (const void *)parent_dev, (const void *)tokens_dev, (const void *)choice_dev,
                           (const void *)path_dev, (const void *)n_accepted_dev, (const void *)next_dev, (const void *)done_out_dev})
         if (!aligned(p, 4))
@@ -380,7 +392,8 @@ static int token_tree_accept_impl(const en_plan *plan, const en_token_rules *rul
     a.chunks = 0;
     if (logits_dev) {
         c.rules = rules ? *rules : en_token_rules{};
-        if ((rc = check_logits(vocab, dtype, logits_dev, logits_stride, who)) != EN_OK || (rc = check_rules(c.rules, vocab, who)) != EN_OK)
+        if ((rc = check_logits(vocab, dtype, logits_dev, logits_stride, who)) != EN_OK || (rc = check_rules(c.rules, vocab, who)) != EN_OK ||
+            (rc = check_grid(plan->B, chunks_of(vocab), who)) != EN_OK)
             return rc;
         const size_t need = en_tree_accept_workspace_bytes(plan, n_nodes, vocab);
         if (!ws_dev || !aligned(ws_dev, 8))

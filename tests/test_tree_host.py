@@ -143,6 +143,17 @@ def test_accept_refusals():
         assert accept(plan, r) == "INVALID_ARG"
 
 
+def test_more_agents_or_tokens_than_a_launch_counts():
+    fine, most = rules(), 65535 * 4096
+    assert apply(fine, agents=65536) == "UNSUPPORTED"
+    assert apply(fine, vocab=most + 1, stride=most + 1, out_stride=most + 1) == "UNSUPPORTED"
+    pool, _ = handles(lens=(1,), cap=1, n_new=1)
+    plan = B.segment_select(pool, [0] * 65536, list(range(65537)), 1)
+    assert accept(plan) == accept(plan, x=None) == commit(pool, plan) == "UNSUPPORTED"
+    _, plan = handles()
+    assert accept(plan, vocab=most + 1, stride=most + 1, ws_bytes=1 << 50) == "UNSUPPORTED"
+
+
 def test_calls_after_the_pool_is_gone():
     pool, plan = handles()
     lib = B.load()
