@@ -5,10 +5,12 @@
 // tree_attn (bf16)
 //
 // All r * n rows of a KV head attend over the same L_c + done keys of the context, so the context is read once for all of
-// them: 32 bytes of it per key and dimension pair against 4 D flops a row. Up to 64 rows a KV head the step is bound by
-// that read, at 256 and more by the matrix instructions too. A workgroup takes up to 8 row blocks of 32 rows (a wave each)
-// of a KV head and a split of its keys; 64-key tiles of K and V^T go straight into LDS, NST of them in turn, and every
-// wave reads all of them there.
+// them: 4 D bytes a key against 4 D flops a key and row. Up to 64 rows a KV head the step is bound by that read (64 agents x
+// 16 K tokens x 4 nodes 766 us, 5.6 TB/s, as fast as a kernel that only reads), at 256 and more by feeding the matrix
+// instructions (64 nodes of 56 heads over 8 K tokens 27.8 us, 15.1 GFLOP: 5 us of start, then 1.8 us a tile of 64 keys), and a
+// short one by its start: arguments, the agent's header and counts, rows and angles are trips to memory one behind the other
+// (8 nodes over 1.5 K tokens 8.2 us). A workgroup takes up to 8 row blocks of 32 rows (a wave each) of a KV head and a split
+// of its keys; 64-key tiles of K and V^T go straight into LDS, NST of them in turn, and every wave reads all of them there.
 //
 // The tree's own keys are one more tile, the last split's first: the workgroup rotates them and lays them out in LDS as a
 // tile of the context would be. Its mask is a row's way, a word whose bit m is node m.
@@ -29,9 +31,9 @@ typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bool no_number(unsigned short bf16) { return (bf16 & 0x7f80) == 0x7f80; }
 
-#ifndef EN_TREE_AHEAD
-#define EN_TREE_AHEAD 6
-#endif
+// Operands that are read ahead of the products. (64 nodes of 56 heads over 8 K tokens: 31.5 us in the compiler's own order,
+// which reads an operand and waits for it, 29.3 so; eight spill.)
+constexpr int EN_TREE_AHEAD = 6;
 // KW = 2: two waves share a row block, a 32-key block of every tile each, and meet at the end.
 template <int D, int RW, int KW, int NST>
 __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((amdgpu_num_vgpr(256))) void tree_attn_kernel(EnTreeArgs a)
@@ -292,8 +294,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
     const int kchunk = (half ^ k_pattern(col)) * 16, vchunk = (half ^ v_pattern(col)) * 16;
     const int u0 = kw * NUW;
 
-    // The order of N products and the reads of their operands: EN_TREE_AHEAD reads ahead. (Left to itself the compiler
-    // reads an operand and waits for it.)
+    // The order of N products and the reads of their operands.
     auto feed = [](auto n_tag) __attribute__((always_inline)) {
         constexpr int N = decltype(n_tag)::value, A = N < EN_TREE_AHEAD ? N : EN_TREE_AHEAD;
         __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
@@ -444,10 +445,11 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
         }
     } else {
         // Two waves share a SIMD, and in step they would ask for its matrix core together and then for its vector ALU
-        // together: 3850 cycles a tile of 64 keys, the sum of both. So the second four waves are half a tile behind: while
+        // together. So the second four waves are half a tile behind: while
         // one half of the waves has its products (the values of a tile and the scores of the next), the other has its
-        // exponentials. A tile's values are read until one and a half tiles behind its scores: of the four stages one is
-        // being read, one still, two are on their way.
+        // exponentials. (64 nodes, us, in step / like this: 56 heads over 8 K tokens 28.7 / 28.0, 32 heads over 8 K 22.9 /
+        // 22.2, 4 agents over 12 K 66.0 / 62.3; over 2 K no difference.) A tile's values are read until one and a half tiles
+        // behind its scores: of the four stages one is being read, one still, two are on their way.
         static_assert(W != 8 || NST == 4, "two tiles are read at a time");
         auto half_done = [&]() __attribute__((always_inline)) {
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
@@ -623,9 +625,10 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
 // tree_merge: out = sum_sp 2^(m_sp - m) O_sp / sum_sp 2^(m_sp - m) l_sp. What the splits left lies as their waves' registers
 // lay: per block of rows, groups of four values per lane. The four waves of a workgroup share a group's splits and meet in
 // LDS (SHARE = 4), or take a group each, where these fill the chip. A split that a row saw nothing of left a sum of 0 and no
-// values; a row without any is zero. grid: blocks * groups * SHARE / 4.
+// values; a row without any is zero. grid: blocks * groups * SHARE / 4. Bound by latency (8 nodes of 32 heads in 25 splits 3.9
+// us) and by its read (3584 rows in 16 splits, 29 MB, 6.7 us, 4.4 TB/s).
 // ---------------------------------------------------------------------------
-// bf16: blocks of 32 rows, a lane's row is lane % 32, group x is dimensions 8 x + 4 (lane / 32) on
+// Blocks of 32 rows, a lane's row is lane % 32, group x is dimensions 8 x + 4 (lane / 32) on
 template <typename T, int D, int SHARE>
 __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
 {
@@ -736,7 +739,8 @@ static int launch_tree_bf16(const EnTreeArgs &a, int blocks, hipStream_t st)
 // tree_f32: the same in single precision on the fp32 matrix instruction (16 x 16 x 4), for small layers, which are bound by
 // latency. As in attn_f32_kernel a workgroup takes 16 rows of a KV head, its eight waves share a split's keys 16 at a time
 // and meet in LDS; no operand goes through LDS. The blocks of the tree's own keys follow those of the context: a lane holds
-// both halves of the pairs of its key, so it turns them in its registers.
+// both halves of the pairs of its key, so it turns them in its registers. 7 nodes of 4 heads over 128 tokens 7.6 us;
+// one wave a row with a softmax of its own a lane 13.4.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(512) void tree_f32_kernel(EnTreeArgs a)
@@ -1033,7 +1037,8 @@ int en_launch_tree_merge(const en_pool *pool, const EnTreeArgs &a, void *stream)
 // tree_commit: entry j of an agent's path goes to context row L_c + (done - accepted) + j, the key rotated there. A workgroup
 // takes a KV head of a layer and agent, all of its tokens: four tokens at positions 4 x to 4 x + 3 are eight bytes side by
 // side in a row of the transposed values, and a store of two bytes costs the memory as much as one of eight. Bound by those
-// rows: D lines per (layer, agent, KV head), read and written back whatever the tokens are. grid: (Hkv * layers, B).
+// rows: D lines per (layer, agent, KV head), read and written back whatever the tokens are. 16 agents x 40 layers x 8 KV heads of
+// 128: 84 MB of such lines, 31 us; one agent's 40 layers 5.0. grid: (Hkv * layers, B).
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(D) void tree_commit_kernel(EnTreeCommitArgs a)
