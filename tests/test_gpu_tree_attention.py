@@ -3,7 +3,7 @@ node's way by itself. Tolerances: tree_cases.near."""
 import numpy as np
 import pytest
 
-from tree_cases import TREES, Tree, chain, comb, near
+from tree_cases import BASE, TREES, Tree, chain, column, comb, near
 
 pytestmark = pytest.mark.gpu
 
@@ -266,3 +266,50 @@ def test_timed_like_the_other_attention_calls():
     torch.cuda.synchronize()
     ms = B.timing_collect(t.pool, 4)
     assert len(ms) == 2 and (ms > 0).all()
+
+
+def test_contexts_of_more_than_4_gib():
+    """The last of 70 agents over 32 K tokens lies 2.3e9 elements into the buffers; its rows and its commit are right, and the
+    other rows of its context are as they were."""
+    import torch
+    from oracle import tree
+    from paper_2510_18546_amd import binding as B
+    agents, kv, d, n, length, n_new = 70, 8, 128, 3, 32_000, 8
+    block = torch.zeros(64, device="cuda:0")
+    pool = B.kv_pool_create(None, None, np.array([length]), kv, BASE, length + n_new, dtype=B.EN_BF16, k_ptr=block.data_ptr(),
+                            v_ptr=block.data_ptr(), shape=(1, kv, length, d))
+    plan = B.segment_select(pool, np.zeros(agents, np.int32), np.arange(agents + 1), n_new)
+    T = plan.info.ctx_stride
+    torch.manual_seed(5)
+    some = dict(dtype=torch.bfloat16, device="cuda:0")
+    kc, vt = torch.zeros(agents, kv, T, d, **some), torch.zeros(agents, kv, d, T, **some)
+    assert kc.numel() > 2**31
+    kc[-1].normal_()
+    vt[-1].normal_()
+    keys = kc[-1].float().cpu().numpy()[None]
+    values = np.moveaxis(vt[-1].float().cpu().numpy()[..., column(np.arange(T))], -1, -2)[None]
+    q, k, v = (torch.randn(agents, n, kv, d, **some) for _ in range(3))
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    parent = torch.tensor([chain(n)] * agents, **i32)
+    done = torch.full((agents,), 2, **i32)
+    out = torch.empty_like(q)
+    ws = torch.empty(max(256, B.tree_workspace_bytes(pool, plan, n)), dtype=torch.uint8, device="cuda:0")
+    B.segmented_tree_attention(pool, plan, done, parent, q, k, v, kc, vt, out, ws)
+    torch.cuda.synchronize()
+    last = [x[-1:].float().cpu().numpy() for x in (q, k, v)]
+    want = tree.attention(keys, values, [length], [2], n_new, parent[-1:].cpu().numpy(), *last, BASE)
+    near(out[-1:].float().cpu().numpy(), want, False)
+
+    path = torch.tensor([[0, 2, -1]] * agents, **i32)
+    B.segmented_tree_commit(pool, plan, done + 2, done, path, [k], [v], [kc], [vt])
+    torch.cuda.synchronize()
+    now = np.moveaxis(vt[-1].float().cpu().numpy()[..., column(np.arange(T))], -1, -2)
+    values[0][:, length + 2:length + 4] = np.moveaxis(last[2][0, [0, 2]], 0, 1)
+    assert np.array_equal(now, values[0])
+    now = kc[-1].float().cpu().numpy()
+    for j, node in ((0, 0), (1, 2)):
+        key = tree.rope(last[1][0, node], length + 2 + j, BASE)
+        # half a step of bf16, and the rotation in float32 as in the tests of the commit
+        assert (np.abs(now[:, length + 2 + j] - key) <= 4 * 2.0 ** -24 * 10 + 2.0 ** -8 * np.abs(key)).all()
+        now[:, length + 2 + j] = keys[0][:, length + 2 + j]
+    assert np.array_equal(now, keys[0])

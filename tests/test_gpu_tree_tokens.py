@@ -127,6 +127,51 @@ def test_rules_leave_what_lies_between_the_rows():
     assert (gaps == 5.0).all() and (buf[:3] == 5.0).all() and (buf[3 + 8 * 1020:] == 5.0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("span", [512, 1024])
+@pytest.mark.parametrize("different", [126, 127, 128, 129, 255, 256, 257, 512])
+def test_rules_where_many_tokens_have_occurred(dtype, span, different):
+    """So many different tokens of the first `span`, some more than once, and ways with tokens that are among them or not."""
+    vocab, n = 5000, 6
+    c = drawn(different, 2, n, vocab, dtype, history=4200, bias="all", mask="node")
+    rng = np.random.default_rng(different)
+    for b in range(2):
+        of = rng.choice(span, min(different, span), replace=False)
+        c["history"][b] = rng.choice(of, 4200)
+        c["history"][b, :len(of)] = of
+        c["tokens"][b] = [of[0], of[0], (of[1] + 1) % span, span, span + 1, of[2]]
+    c["history_len"][:] = [4200, 99999]
+    check_rules(c, forest(2, n), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rules_count_a_token_as_often_as_the_way_has_it(dtype):
+    c = drawn(4, 2, 64, 700, dtype, 0)
+    c["tokens"][:] = 5
+    c["tokens"][1, ::2] = 699
+    check_rules(c, np.stack([chain(64), comb(64)]).astype(np.int32), dtype)
+
+
+def test_logits_further_apart_than_2_to_the_31():
+    """64 rows of a tensor of 2.6e9 elements."""
+    import torch
+    from oracle import tree
+    from paper_2510_18546_amd import binding as B
+    n, vocab, apart = 64, 1000, 41_000_003
+    c = drawn(6, 1, n, vocab, "bf16", 30, exact=True)
+    parent = comb(n)[None].astype(np.int32)
+    x = torch.empty(n * apart, dtype=torch.bfloat16, device="cuda:0").as_strided((1, n, vocab), (n * apart, apart, 1))
+    x.copy_(dev(c["logits"]))
+    t = Tree(2, "bf16", [4], [0], 80, parent, d=64)
+    choice = accepted(t, c["tokens"], x, rules_of(c))[0]
+    B.token_rules_apply(rules_of(c), x, x, dev(parent), dev(c["tokens"]))
+    torch.cuda.synchronize()
+    want = tree.rules(c["logits"], parent, c["tokens"], *(c[k] for k in RULES))
+    assert list(choice[0]) == [tree.choose(row) for row in want[0]]
+    # (exact in float32, rounded to bf16 once)
+    assert np.array_equal(x.float().cpu().numpy(), bf16(want))
+
+
 def accepted(t, tokens, logits, rules=None, choice="out", ws=None, done_out=None):
     import torch
     from paper_2510_18546_amd import binding as B
@@ -181,6 +226,18 @@ def test_accept(dtype, n, vocab, history, bias, mask):
     c = drawn(vocab, agents, n, vocab, dtype, history, bias, mask, exact=True)
     agree(c, t, rng)
     check_accept(t, c, dtype, pad=vocab % 3, shift=vocab % 2)
+
+
+@pytest.mark.parametrize("different", [255, 256, 257])
+def test_accept_where_many_tokens_have_occurred(different):
+    c = drawn(different, 2, 9, 3000, "f32", 3000, None, "agent", exact=True)
+    rng = np.random.default_rng(1)
+    for b in range(2):
+        c["history"][b] = rng.choice(rng.choice(1024, different, replace=False), 3000)
+    c["history_len"][:] = 3000
+    t = Tree(9, "bf16", [10] * 2, [0, 5], 80, forest(2, 9), d=64)
+    agree(c, t, rng)
+    check_accept(t, c, "f32")
 
 
 def test_accept_goes_deep():
