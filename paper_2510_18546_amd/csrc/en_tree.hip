@@ -18,9 +18,13 @@
 // S^T = K Q^T and O^T += V^T P^T with 32 x 32 x 16 products as in attn_decode_kernel: a lane's column is a query row, its
 // scores of 16 keys of a 32-key block are the operand of the second product as they are (that is what the exchanged bits
 // 2 and 3 of a value's column are for). Scores are in log2 units, taken against a reference that is the maximum of the
-// first keys a row sees and changes only where a score is 2^59 above it. The queries, the drafted keys, the probabilities
-// and the output are rounded to bf16 once each (what the products take); sums, references and what the splits leave for
-// the merge are float32.
+// first keys a row sees and changes only where a score is 2^59 above it. The drafted keys, the probabilities and the output
+// are rounded to bf16 once each (what the products take); sums, references and what the splits leave for the merge are
+// float32. A query is the sum of two bf16 numbers, its rounding and what that left, where up to four blocks of rows share a
+// tile, and is rounded once where eight do: the second product of its scores would be half as much again of what those steps
+// are bound by. (Outputs' error against 64 bits, 2-norm, 0.0021 / 0.0028, of which the output's own rounding is 0.0017. Two
+// parts / one, us: 8 nodes over 1.5 K tokens 8.7 / 8.2, 16 agents with 13 nodes over 2 K 32.4 / 30.6, 64 agents over 16 K
+// 772 / 771, 4 agents with 32 nodes over 4 K 26.1 / 24.1; 64 nodes of 56 heads over 8 K 35.0 in blocks of four / 28.0.)
 //
 // 16-byte chunks of a row lie in LDS exchanged by XOR with its number, so that 16 consecutive rows' reads of the same
 // chunk meet distinct banks; the loads bring them there by reading their source in that order.
@@ -39,6 +43,7 @@ template <int D, int RW, int KW, int NST>
 __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((amdgpu_num_vgpr(256))) void tree_attn_kernel(EnTreeArgs a)
 {
     constexpr int W = RW * KW;
+    constexpr bool TWO_PARTS = W < 8;            // of the queries, see above
     constexpr int NT = 64 * W;                   // threads
     constexpr int KB = 32;                       // keys per matrix-instruction block
     constexpr int LB = EN_KEY_TILE;              // keys per tile
@@ -178,7 +183,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
     const unsigned long long way = __shfl(tree.way, i_row, 64);
     const int depth = __shfl(tree.depth, i_row, 64);
     const bool row_valid = row_there && way != 0;
-    bf16x8 qf[NKS];
+    bf16x8 qf[NKS], ql[TWO_PARTS ? NKS : 1];         // the query, and what its rounding left
     f32x8 t_cs, t_sn;                            // of the tree's keys
     auto tree_angles = [&](int m) __attribute__((always_inline)) {
         const int d_m = __popcll(__shfl(tree.way, m, 64)) - 1;
@@ -219,13 +224,21 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
             for (int j = 0; j < 8; ++j) {
                 const float x1 = (float)qraw[ks][j], x2 = (float)qraw[ks + NKS / 2][j];
                 const float c = cs[ks][j] * scale, s = sn[ks][j] * scale;
-                qf[ks][j] = (bf16_t)(x1 * c - x2 * s);
-                qf[ks + NKS / 2][j] = (bf16_t)(x2 * c + x1 * s);
+                const float y1 = x1 * c - x2 * s, y2 = x2 * c + x1 * s;
+                qf[ks][j] = (bf16_t)y1;
+                qf[ks + NKS / 2][j] = (bf16_t)y2;
+                if constexpr (TWO_PARTS) {
+                    ql[ks][j] = (bf16_t)(y1 - (float)qf[ks][j]);
+                    ql[ks + NKS / 2][j] = (bf16_t)(y2 - (float)qf[ks + NKS / 2][j]);
+                }
             }
         if (!row_valid)                          // (what such a row holds may be no number)
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks)
+            for (int ks = 0; ks < NKS; ++ks) {
                 qf[ks] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                if constexpr (TWO_PARTS)
+                    ql[ks] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            }
     }
 
     // ---- the tree's tile into stage 0. Keys of absent nodes may stay what they are (nobody sees their scores), their
@@ -296,13 +309,13 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
 
     // The order of N products and the reads of their operands.
     auto feed = [](auto n_tag) __attribute__((always_inline)) {
-        constexpr int N = decltype(n_tag)::value, A = N < EN_TREE_AHEAD ? N : EN_TREE_AHEAD;
+        constexpr int N = decltype(n_tag)::value, A = N < EN_TREE_AHEAD ? N : EN_TREE_AHEAD, EACH = TWO_PARTS ? 2 : 1;
         __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
         static_for<N - A>([](auto) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         });
-        __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, A * EACH, 0);
     };
 
     // ---- a tile in three pieces: scores, probabilities, values; iteration `it` of the workgroup's ----
@@ -318,6 +331,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
             for (int u = 0; u < NUW; ++u) {
                 const bf16x8 fr = *reinterpret_cast<const bf16x8 *>(stg + ((u0 + u) * KB + col) * ROWB + (kchunk ^ (32 * ks)));
                 sv[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, qf[ks], ks == 0 ? negm : sv[u], 0, 0, 0);
+                if constexpr (TWO_PARTS)
+                    sv[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, ql[ks], sv[u], 0, 0, 0);
             }
     };
     auto probability_block = [&](int u) __attribute__((always_inline)) {
