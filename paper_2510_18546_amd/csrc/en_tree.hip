@@ -727,6 +727,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(EnTreeArgs a)
 template <typename T, int D>
 static void launch_merge(const EnTreeArgs &a, hipStream_t st)
 {
+    // Four waves to a group / one, us: 128 groups of 25 splits 3.9 / 5.8, 512 of 32 5.0 / 6.9, 1792 of 16 6.8 / 6.8, 2048 of 8
+    // 5.4 / 5.3, 4096 of 8 7.9 / 7.6, 4096 of 4 8.4 / 6.3, 8192 of 4 14.9 / 12.0.
     const unsigned items = a.n_blocks * (D / 8);
     if (items < 2048)
         hipLaunchKernelGGL((tree_merge_kernel<T, D, 4>), dim3((items + EN_XCDS - 1) / EN_XCDS * EN_XCDS), dim3(256), 0, st, a);

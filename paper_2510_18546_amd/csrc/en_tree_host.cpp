@@ -80,6 +80,8 @@ static TreeCut tree_cut(const en_pool *pool, const en_plan *plan, int n)
         c.blocks *= 2;
     c.n_ptiles = (all + c.blocks - 1) / c.blocks;
     c.tile_blocks = (all + c.n_ptiles - 1) / c.n_ptiles;
+    // (Its start included, the tree's tile of eight blocks takes as long as two: counted as one / two, 64 nodes of 56 heads over
+    // 8 K tokens 29.0 / 28.0 us, over 2 K 18.0 / 17.2, of 32 heads over 8 K 22.2 / 22.0.)
     c.tree_tiles = c.blocks == EN_TREE_BLOCKS ? 2 : 1;
     const long units = long(plan->B) * pool->d.n_kv_heads * c.n_ptiles;
     const int tiles = (plan->max_ctx_len + EN_KEY_TILE - 1) / EN_KEY_TILE + 1;

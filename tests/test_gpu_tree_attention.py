@@ -290,7 +290,7 @@ def test_contexts_of_more_than_4_gib():
     values = np.moveaxis(vt[-1].float().cpu().numpy()[..., column(np.arange(T))], -1, -2)[None]
     q, k, v = (torch.randn(agents, n, kv, d, **some) for _ in range(3))
     i32 = dict(dtype=torch.int32, device="cuda:0")
-    parent = torch.tensor([chain(n)] * agents, **i32)
+    parent = torch.tensor(np.stack([chain(n)] * agents), **i32)
     done = torch.full((agents,), 2, **i32)
     out = torch.empty_like(q)
     ws = torch.empty(max(256, B.tree_workspace_bytes(pool, plan, n)), dtype=torch.uint8, device="cuda:0")
