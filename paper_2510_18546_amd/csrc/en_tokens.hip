@@ -45,7 +45,7 @@ __device__ __forceinline__ void wave_lds_order()
 // row: 16 a lane, in two runs of eight, or one run. Reading the logits once (and writing them once) is all that choices
 // without rules cost: 64 x 32 rows of 128000 tokens, bf16, 91 us, 5.8 TB/s; one agent's eight rows of 32000 3.8, which is a
 // launch and two trips to memory. Under penalties the tables' set-up comes first (7 us with 2 - 4 K tokens of history), then
-// the instructions a token: all rules on 16 x 13 rows of 50021 tokens 18.2 us, choices of 128000 under all rules 25.8.
+// the instructions a token: all rules on 16 x 13 rows of 50021 tokens 17.7 us, choices of 128000 under all rules 25.9.
 //
 // The tokens that penalties concern are few: they are counted into a table in LDS once for all rows of the workgroup, each
 // wave lists those of its share, and in a row only they are divided and subtracted from, in a copy of the share in
@@ -65,16 +65,22 @@ struct EnRulesLds {
     unsigned short hit[EN_RULES_CHUNK / 4];
 };
 
-// Rules that are written out take eight waves with half as many tokens each: 16 agents' 13 rows of 50021 tokens 19.1 us with
-// four, 18.2 with eight, one row of 32000 6.1 / 5.2. Choices have a wave's exchanges for each row besides: 16 x 13 rows of
-// 128000 tokens under all rules 25.8 / 27.2.
-constexpr int en_rules_waves(bool choose, bool ruled) { return ruled && !choose ? 8 : 4; }
+// RULES: none, a bias or a mask, or penalties too. (One instance for all rules, which keeps 128 registers and half as many waves
+// where there are no penalties: choices of 64 x 32 rows of 128000 tokens under a bias and masks 161 us, now 110, of 16 x 13 18.5 /
+// 17.0; 16 x 13 rows of 50021 written out 13.1 / 12.8.)
+enum EnRulesKind { EN_NO_RULES, EN_FEW_RULES, EN_ALL_RULES };
 
-// RULED: there may be penalties, a bias or a mask.
-template <typename T, bool CHOOSE, bool RULED>
-__global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rules_waves(CHOOSE, RULED) : 1) void rules_kernel(EnRulesArgs a)
+// Rules that are written out take eight waves with half as many tokens each: 16 agents' 13 rows of 50021 tokens under all rules
+// 19.1 us with four, 18.2 with eight, under masks 13.1 / 11.4, one row of 32000 6.1 / 5.2. Choices have a wave's exchanges for
+// each row besides: 16 x 13 rows of 128000 tokens under all rules 25.8 / 27.2, under masks 16.2 / 17.6.
+constexpr int en_rules_waves(bool choose, int rules) { return rules != EN_NO_RULES && !choose ? 8 : 4; }
+
+template <typename T, bool CHOOSE, int RULES>
+__global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULES), RULES == EN_NO_RULES ? 1 : RULES == EN_ALL_RULES && CHOOSE ? 4 : 8)
+void rules_kernel(EnRulesArgs a)
 {
-    constexpr int WAVES = en_rules_waves(CHOOSE, RULED), NT = 64 * WAVES;
+    constexpr bool RULED = RULES != EN_NO_RULES, PENALTIES = RULES == EN_ALL_RULES;
+    constexpr int WAVES = en_rules_waves(CHOOSE, RULES), NT = 64 * WAVES;
     constexpr int WAVE_TOKENS = EN_RULES_CHUNK / WAVES;
     constexpr int Q = WAVE_TOKENS / 512;                 // runs of eight a lane
     constexpr int LISTED = WAVE_TOKENS / 4;              // of so many tokens that have occurred a list is worth its trips through LDS
@@ -89,11 +95,10 @@ __global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rule
     // what is asked for first, in one trip: the history's first entries (as many as there may be: how many there are is on
     // its way too), the penalties, the tree's tokens
     constexpr int HJ = 8;
-    const bool penalties_on = RULED && r.penalties_dev;
     const int *const history = r.history_dev ? r.history_dev + (size_t)b * r.history_stride : nullptr;
     int early[HJ], token = -1, h = 0;
     float rep = 1.f, freq = 0.f, pres = 0.f;
-    if (penalties_on) {
+    if constexpr (PENALTIES) {
         const int most = history ? r.history_stride : 0;
 #pragma unroll
         for (int j = 0; j < HJ; ++j)
@@ -168,7 +173,7 @@ __global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rule
     int n_hit = 0, my_token = -1;                        // my_token: of node `lane`, in the share, or -1
     int *const count = lds.count + wave * WAVE_TOKENS;
     unsigned short *const hit = lds.hit + wave * LISTED;
-    if (penalties_on) {
+    if constexpr (PENALTIES) {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int k = 0; k < EN_RULES_CHUNK / (4 * NT); ++k)
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rule
         }
         wave_lds_order();
     }
-    const unsigned long long in_share = RULED ? __ballot(my_token >= 0) : 0ull;
+    const unsigned long long in_share = PENALTIES ? __ballot(my_token >= 0) : 0ull;
 
     auto penalties = [&](float (&x)[Q][8], unsigned long long way) __attribute__((always_inline)) {
         const bool own = (way & in_share) != 0;
@@ -272,7 +277,7 @@ __global__ __launch_bounds__(64 * en_rules_waves(CHOOSE, RULED), RULED ? en_rule
             for (int j = 0; j < 8; ++j)
                 x[q][j] = (float)in.run[q].x[j];
         if constexpr (RULED) {
-            if (penalties_on)
+            if constexpr (PENALTIES)
                 penalties(x, a.parent ? readlane64(tree.way, i) : 0ull);
             if (bias)
 #pragma unroll
@@ -411,16 +416,21 @@ __global__ __launch_bounds__(1024) void accept_kernel(EnAcceptArgs a)
     }
 }
 
+template <typename T, bool CHOOSE, int RULES>
+static int launch_rules_kernel(const EnRulesArgs &a, hipStream_t st)
+{
+    const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks);
+    hipLaunchKernelGGL((rules_kernel<T, CHOOSE, RULES>), grid, dim3(64 * en_rules_waves(CHOOSE, RULES)),
+                       RULES == EN_ALL_RULES ? sizeof(EnRulesLds) : 0, st, a);
+    return (int)hipGetLastError();
+}
 template <typename T, bool CHOOSE>
 static int launch_rules(const EnRulesArgs &a, hipStream_t st)
 {
-    const dim3 grid((a.n + a.nodes - 1) / a.nodes, a.B, a.chunks);
-    const size_t lds = a.rules.penalties_dev ? sizeof(EnRulesLds) : 0;
-    if (a.rules.penalties_dev || a.rules.bias_dev || a.rules.mask_dev)
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, true>), grid, dim3(64 * en_rules_waves(CHOOSE, true)), lds, st, a);
-    else
-        hipLaunchKernelGGL((rules_kernel<T, CHOOSE, false>), grid, dim3(64 * en_rules_waves(CHOOSE, false)), 0, st, a);
-    return (int)hipGetLastError();
+    if (a.rules.penalties_dev)
+        return launch_rules_kernel<T, CHOOSE, EN_ALL_RULES>(a, st);
+    return a.rules.bias_dev || a.rules.mask_dev ? launch_rules_kernel<T, CHOOSE, EN_FEW_RULES>(a, st)
+                                                : launch_rules_kernel<T, CHOOSE, EN_NO_RULES>(a, st);
 }
 int en_launch_rules(const EnRulesArgs &a, int dtype, void *stream)
 {
