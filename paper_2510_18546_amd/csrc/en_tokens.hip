@@ -296,14 +296,16 @@ void rules_kernel(EnRulesArgs a)
         }
         if constexpr (CHOOSE) {
             // The largest of each run, of the wave, the first lane that has it in its first run or else in its second, and
-            // which of the run's it is: of equals the lowest token. (NaN is no maximum.)
+            // which of the run's it is: of equals the lowest token. (NaN is no maximum. A maximum passes over a quiet NaN, but
+            // of a signalling one, which logits may hold as they come from memory, the hardware makes NaN: canonical numbers
+            // are quiet.)
             float top_of[Q];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 top_of[q] = EN_NEG_INF;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    top_of[q] = fmaxf(top_of[q], x[q][j]);
+                    top_of[q] = fmaxf(top_of[q], __builtin_canonicalizef(x[q][j]));
             }
             const float top = wave_max(fmaxf(top_of[0], top_of[Q - 1]));
             const unsigned long long in0 = __ballot(top_of[0] == top), in1 = __ballot(top_of[Q - 1] == top);

@@ -275,6 +275,71 @@ def test_accept_ties_zeros_and_what_is_no_number(dtype):
     assert list(choice[:, 0]) == want and list(token) == want and (count == 1).all() and (path[:, 0] == 0).all() and (done == 1).all()
 
 
+def put_signalling(view, at, sign):
+    """Signalling NaN, which no arithmetic brings forth, into logits on the device."""
+    import torch
+    if view.dtype == torch.float32:
+        view.view(torch.int32)[at] = 0x7F800001 - (2**31 if sign else 0)
+    else:
+        view.view(torch.int16)[at] = 0x7F81 - (2**15 if sign else 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [0, 1])
+@pytest.mark.parametrize("ruled", ["none", "mask", "penalties", "bias"])
+@pytest.mark.parametrize("vocab,base", [(3000, 1480), (3000, 2992), (2053, 2045), (5000, 600)])
+def test_accept_signalling_nan(dtype, sign, ruled, vocab, base):
+    """The largest logit at every place of a run of eight, a signalling NaN at every other one."""
+    places = [(i, j) for i in range(8) for j in range(8) if i != j]
+    agents = len(places)
+    t = Tree(1, "bf16", [4] * agents, [0] * agents, 4, [[-1]] * agents, d=64)
+    c = drawn(3, agents, 1, vocab, dtype, 0 if ruled == "penalties" else None, "all" if ruled == "bias" else None)
+    c["logits"][:] = -5.0
+    c["tokens"][:] = 17
+    if ruled == "mask":
+        c["mask"] = np.full((agents, 1, (vocab + 31) // 32), -1, np.int32)
+    if ruled == "bias":
+        c["bias"][:] = 0.25
+    for b, (i, _) in enumerate(places):
+        c["logits"][b, 0, base + i] = 2.0
+    x = logits_on(c["logits"], dtype)
+    for b, (_, j) in enumerate(places):
+        put_signalling(x, (b, 0, base + j), sign)
+    choice, _, _, token, _ = accepted(t, c["tokens"], x, rules_of(c) if ruled != "none" else None)
+    want = [base + i for i, _ in places]
+    assert list(choice[:, 0]) == want and list(token) == want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_accept_signalling_nan_everywhere(dtype):
+    vocab = 2500
+    t = Tree(1, "bf16", [4] * 2, [0] * 2, 4, [[-1]] * 2, d=64)
+    x = logits_on(np.zeros((2, 1, vocab), np.float32), dtype)
+    put_signalling(x, slice(None), 0)
+    x[1, 0, 1234] = -3.0
+    choice = accepted(t, np.zeros((2, 1), np.int32), x)[0]
+    assert list(choice[:, 0]) == [-1, 1234]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ruled", ["mask", "penalties"])
+def test_rules_signalling_nan_stays_nan(dtype, ruled):
+    """Written out it is still no number, unless the mask hides it; its neighbours are what they are."""
+    import torch
+    from oracle import tree
+    from paper_2510_18546_amd import binding as B
+    c = drawn(7, 2, 1, 1500, dtype, 0 if ruled == "penalties" else None, None, "agent" if ruled == "mask" else None)
+    at = np.array([0, 3, 511, 700, 1499])
+    x = logits_on(c["logits"], dtype)
+    put_signalling(x, (slice(None), slice(None), torch.tensor(at, device="cuda:0")), 0)
+    c["logits"][..., at] = np.nan
+    out = torch.empty_like(x)
+    B.token_rules_apply(rules_of(c), x, out)
+    torch.cuda.synchronize()
+    want = tree.rules(c["logits"], None, None, *(c[k] for k in RULES))
+    assert np.array_equal(out.double().cpu().numpy(), want, equal_nan=True)
+
+
 def test_accept_where_a_mask_leaves_nothing():
     t = Tree(1, "bf16", [4] * 2, [0] * 2, 8, [chain(3)] * 2, d=64)
     c = drawn(2, 2, 3, 300, "f32", None, None, "node", exact=True)
