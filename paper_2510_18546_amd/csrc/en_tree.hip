@@ -20,8 +20,8 @@
 // 2 and 3 of a value's column are for). Scores are in log2 units, taken against a reference that is the maximum of the
 // first keys a row sees and changes only where a score is 2^59 above it. The drafted keys, the probabilities and the output
 // are rounded to bf16 once each (what the products take); sums, references and what the splits leave for the merge are
-// float32. A query is the sum of two bf16 numbers, its rounding and what that left, where up to four blocks of rows share a
-// tile, and is rounded once where eight do: the second product of its scores would be half as much again of what those steps
+// float32. A query is the sum of two bf16 numbers (see cut_off) where up to four blocks of rows share a tile, and is rounded
+// once where eight do: the second product of its scores would be half as much again of what those steps
 // are bound by. (Outputs' error against 64 bits, 2-norm, 0.0021 / 0.0028, of which the output's own rounding is 0.0017. Two
 // parts / one, us: 8 nodes over 1.5 K tokens 8.7 / 8.2, 16 agents with 13 nodes over 2 K 32.4 / 30.6, 64 agents over 16 K
 // 772 / 771, 4 agents with 32 nodes over 4 K 26.1 / 24.1; 64 nodes of 56 heads over 8 K 35.0 in blocks of four / 28.0.)
@@ -34,6 +34,17 @@
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bool no_number(unsigned short bf16) { return (bf16 & 0x7f80) == 0x7f80; }
+
+// A query's two parts have one sign and neither is zero, unless the query is: against a key that is infinite both products
+// are the same infinity, and a score of minus infinity is no weight, where an infinity times zero, or two of different signs,
+// were NaN. So the first part is cut off, not rounded (what is left is below 2^-7 of it, and its rounding below 2^-15), and the
+// second is the smallest normal number where nothing is left.
+__device__ __forceinline__ float cut_off(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ bf16x8 with_sign_of(bf16x8 v, bf16x8 of)
+{
+    const u16x8 a = __builtin_bit_cast(u16x8, v) & (unsigned short)0x7fff, least = (unsigned short)0x0080;
+    return __builtin_bit_cast(bf16x8, __builtin_elementwise_max(a, least) | (__builtin_bit_cast(u16x8, of) & (unsigned short)0x8000));
+}
 
 // Operands that are read ahead of the products. (64 nodes of 56 heads over 8 K tokens: 31.5 us in the compiler's own order,
 // which reads an operand and waits for it, 29.3 so; eight spill.)
@@ -225,13 +236,20 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
                 const float x1 = (float)qraw[ks][j], x2 = (float)qraw[ks + NKS / 2][j];
                 const float c = cs[ks][j] * scale, s = sn[ks][j] * scale;
                 const float y1 = x1 * c - x2 * s, y2 = x2 * c + x1 * s;
-                qf[ks][j] = (bf16_t)y1;
-                qf[ks + NKS / 2][j] = (bf16_t)y2;
                 if constexpr (TWO_PARTS) {
-                    ql[ks][j] = (bf16_t)(y1 - (float)qf[ks][j]);
-                    ql[ks + NKS / 2][j] = (bf16_t)(y2 - (float)qf[ks + NKS / 2][j]);
+                    ql[ks][j] = (bf16_t)(y1 - cut_off(y1));
+                    ql[ks + NKS / 2][j] = (bf16_t)(y2 - cut_off(y2));
+                    qf[ks][j] = (bf16_t)cut_off(y1);
+                    qf[ks + NKS / 2][j] = (bf16_t)cut_off(y2);
+                } else {
+                    qf[ks][j] = (bf16_t)y1;
+                    qf[ks + NKS / 2][j] = (bf16_t)y2;
                 }
             }
+        if constexpr (TWO_PARTS)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+                ql[ks] = with_sign_of(ql[ks], qf[ks]);
         if (!row_valid)                          // (what such a row holds may be no number)
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) {

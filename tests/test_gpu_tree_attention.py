@@ -3,7 +3,7 @@ node's way by itself. Tolerances: tree_cases.near."""
 import numpy as np
 import pytest
 
-from tree_cases import BASE, TREES, Tree, chain, column, comb, near
+from tree_cases import BASE, TREES, Tree, bf16, chain, column, comb, near
 
 pytestmark = pytest.mark.gpu
 
@@ -98,6 +98,30 @@ def test_rows_that_are_no_numbers_reach_their_descendants_only(dtype, value, n, 
             assert not np.isfinite(got[b][dirty][..., ::3]).any()
             rest = np.arange(t.d) % 3 != 0
             near(got[b, dirty][..., rest], want[b, dirty][..., rest], t.f32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,r,d", [(9, 3, 64), (4, 2, 128), (13, 4, 128), (32, 4, 64), (64, 2, 128), (64, 7, 128), (64, 4, 64)])
+def test_visible_keys_of_minus_infinity_have_no_weight(dtype, n, r, d):
+    """A key with a component of minus infinity where the query's is positive has a score of minus infinity: it takes no
+    part, and the rows that see it are finite. In the context, and in the tree, where the turned key is minus infinity in
+    both halves of its pair. (The pair is the slowest one, which no position here turns by more than 0.001.)"""
+    import torch
+    t = Tree(n, dtype, [150, 70], [0, 3], 80, [comb(n), comb(n)], r=r, kv=1, d=d)
+    first, second = d // 2 - 1, d - 1
+    for half in (first, second):
+        t.q[..., half] = np.abs(t.q[..., half]) + 0.5
+    if not t.f32:
+        t.q = bf16(t.q)
+    t.keys[0][0, 0, [3, 64, 149], first] = -np.inf
+    t.keys[0][1, 0, [0, 72], second] = -np.inf
+    t.k[0][1, min(n - 1, 2), 0, first] = -np.inf
+    t.up()
+    t.kc = [t.device(x) for x in t.keys]
+    got, want = t.attend(), t.expected()
+    torch.cuda.synchronize()
+    assert np.isfinite(want).all()
+    near(got.float().cpu().numpy(), want, t.f32)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
