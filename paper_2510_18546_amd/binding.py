@@ -476,15 +476,31 @@ def _buffer(name: str, t, nbytes: int, dev: int) -> int:
     return t.data_ptr()
 
 
-def _all_at(name: str, ts, nbytes: int, dtype, dev: int, exact: bool) -> array.array:
-    """Addresses of the layers' tensors, contiguous, of (`exact`) or of at least that many bytes, on the device."""
+def _context(name: str, t, nbytes: int, dtype, dev: int) -> int:
+    """Address of a context buffer, numbers of that type or bare bytes (as alloc_context makes them)."""
+    if t.dtype is not dtype and t.dtype.is_floating_point:
+        raise _unfit(name, t, f"a context of {dtype}")
+    return _buffer(name, t, nbytes, dev)
+
+
+def _layers_rows(name: str, ts, shape: tuple, dtype, dev: int) -> array.array:
+    """Addresses of the layers' rows, contiguous tensors of that shape and type on the device."""
     t_ = _torch().Tensor
-    sizes = set(map(t_.nbytes.__get__, ts))
-    if (min(sizes) < nbytes or exact and (max(sizes) != nbytes or set(map(t_.dtype.__get__, ts)) != {dtype}) or
+    if not (list(map(t_.shape.__get__, ts)).count(shape) == len(ts) and set(map(t_.dtype.__get__, ts)) == {dtype} and
+            all(map(t_.is_contiguous, ts)) and set(map(t_.get_device, ts)) == {dev}):
+        raise ValueError(f"{name}: a contiguous {shape} of {dtype} on the current device is wanted for every layer")
+    return array.array("Q", list(map(t_.data_ptr, ts)))
+
+
+def _layers_contexts(name: str, ts, nbytes: int, dtype, dev: int) -> array.array:
+    """Addresses of the layers' contexts (see _context)."""
+    t_ = _torch().Tensor
+    types = set(map(t_.dtype.__get__, ts))
+    if (min(map(t_.nbytes.__get__, ts)) < nbytes or types != {dtype} and any(x is not dtype and x.is_floating_point for x in types) or
             not all(map(t_.is_contiguous, ts)) or set(map(t_.get_device, ts)) != {dev}):
-        raise ValueError(f"{name}: a contiguous tensor of {'' if exact else 'at least '}{nbytes} bytes{f' of {dtype}' if exact else ''} on "
-                         "the current device is wanted for every layer")
-    return array.array("Q", map(t_.data_ptr, ts))
+        raise ValueError(f"{name}: a contiguous context of at least {nbytes} bytes, {dtype} or bytes, on the current device is wanted "
+                         "for every layer")
+    return array.array("Q", list(map(t_.data_ptr, ts)))
 
 
 _torch_module = None
@@ -507,7 +523,8 @@ def tree_workspace_bytes(pool: Pool, plan: Plan, n_nodes: int) -> int:
 
 
 def segmented_tree_attention(pool: Pool, plan: Plan, done, parent, q, k_rows, v_rows, kc, vt, out, ws=None, stream=None):
-    """done int32 [B], parent int32 [B, n]; q, out [B, n, Hq, D], k_rows/v_rows [B, n, Hkv, D] in the contexts' type."""
+    """done int32 [B], parent int32 [B, n]; q, out [B, n, Hq, D], k_rows/v_rows [B, n, Hkv, D] in the contexts' type; kc, vt
+    context buffers, of that type or of bytes."""
     lib, i32, t, dev, d = load(), _torch().int32, _row_type(pool.desc), _device(), pool.desc
     b, n = parent.shape
     if b != plan.n_agents:
@@ -516,7 +533,7 @@ def segmented_tree_attention(pool: Pool, plan: Plan, done, parent, q, k_rows, v_
     _check(lib.segmented_tree_attention(
         pool.handle, plan.handle, n, _at("done", done, (b,), i32, dev), _at("parent", parent, (b, n), i32, dev),
         _at("q", q, rows, t, dev), _at("k_rows", k_rows, mine, t, dev), _at("v_rows", v_rows, mine, t, dev),
-        _buffer("kc", kc, ctx, dev), _buffer("vt", vt, ctx, dev), _at("out", out, rows, t, dev),
+        _context("kc", kc, ctx, t, dev), _context("vt", vt, ctx, t, dev), _at("out", out, rows, t, dev),
         _buffer("ws", ws, 0, dev) if ws is not None else None, ws.nbytes if ws is not None else 0, _stream(stream)))
     return out
 
@@ -627,7 +644,7 @@ def token_tree_accept(plan: Plan, done, parent, tokens, logits, choice, path, n_
 
 def segmented_tree_commit(pool: Pool, plan: Plan, done, n_accepted, path, k_rows, v_rows, kc, vt, stream=None):
     """done (after the acceptance), n_accepted int32 [B], path int32 [B, n]; k_rows, v_rows: a tensor [B, n, Hkv, D] per
-    layer, kc, vt: a context buffer per layer."""
+    layer, kc, vt: a context buffer per layer, in the type of the rows or of bytes."""
     lib, i32, dev, d, t = load(), _torch().int32, _device(), pool.desc, _row_type(pool.desc)
     b, n = path.shape
     if b != plan.n_agents:
@@ -637,9 +654,9 @@ def segmented_tree_commit(pool: Pool, plan: Plan, done, n_accepted, path, k_rows
         raise ValueError(f"{layers}, {len(v_rows)}, {len(kc)}, {len(vt)} layers")
     if layers == 0:
         return
-    mine, ctx = b * n * d.n_kv_heads * d.head_dim * t.itemsize, plan.context_bytes
-    ptrs = [_all_at("k_rows", k_rows, mine, t, dev, True), _all_at("v_rows", v_rows, mine, t, dev, True),
-            _all_at("kc", kc, ctx, t, dev, False), _all_at("vt", vt, ctx, t, dev, False)]
+    mine, ctx = (b, n, d.n_kv_heads, d.head_dim), plan.context_bytes
+    ptrs = [_layers_rows("k_rows", k_rows, mine, t, dev), _layers_rows("v_rows", v_rows, mine, t, dev),
+            _layers_contexts("kc", kc, ctx, t, dev), _layers_contexts("vt", vt, ctx, t, dev)]
     _check(lib.segmented_tree_commit(
         pool.handle, plan.handle, n, layers, _at("done", done, (b,), i32, dev), _at("n_accepted", n_accepted, (b,), i32, dev),
         _at("path", path, (b, n), i32, dev), *(p.buffer_info()[0] for p in ptrs), _stream(stream)))

@@ -176,6 +176,75 @@ def test_binding_refusals():
             B.token_rules(**kw)
 
 
+def layered(monkeypatch):
+    """Calls of the binding up to the library, whose part takes everything: (pool, plan, the right arguments)."""
+    import types
+
+    import torch
+    pool, plan = handles(lens=(30, 5), d=64, hkv=2, hq=4)
+    ctx = plan.context_bytes
+    taken = types.SimpleNamespace(segmented_tree_commit=lambda *a: 0, segmented_tree_attention=lambda *a: 0)
+    monkeypatch.setattr(B, "load", lambda path=None: taken)
+    monkeypatch.setattr(B, "_device", lambda: -1)            # (a CPU tensor's)
+    some = dict(dtype=torch.bfloat16)
+    return pool, plan, ctx, dict(rows=[torch.zeros(2, 3, 2, 64, **some) for _ in range(3)],
+                                 contexts=[torch.zeros(ctx // 2, **some) for _ in range(3)], ints=torch.zeros(2, dtype=torch.int32),
+                                 tree=torch.zeros(2, 3, dtype=torch.int32), q=torch.zeros(2, 3, 4, 64, **some))
+
+
+def unfit_rows(x):
+    """The same bytes as rows [B, n, Hkv, D], or as many, that are none."""
+    import torch
+    b, n, h, d = x.shape
+    return [x.transpose(1, 2).contiguous(), x.view(b, n, h * d), x.view(b * n, h, d), x.to(torch.float16), x.view(torch.int16),
+            torch.zeros(b, n, h, 2 * d, dtype=x.dtype)[..., :d], x[:, :2].contiguous()]
+
+
+def unfit_contexts(x):
+    import torch
+    return [x.float(), x.to(torch.float16), x.double(), x[:-1], torch.zeros(x.numel(), 2, dtype=x.dtype)[:, 0]]
+
+
+def test_binding_commit_looks_at_shape_and_type_of_every_layer(monkeypatch):
+    pool, plan, _, a = layered(monkeypatch)
+
+    def commit(**other):
+        x = {"k": list(a["rows"]), "v": list(a["rows"]), "kc": list(a["contexts"]), "vt": list(a["contexts"])}
+        for name, tensor in other.items():
+            x[name][1] = tensor
+        B.segmented_tree_commit(pool, plan, a["ints"], a["ints"], a["tree"], x["k"], x["v"], x["kc"], x["vt"], stream=0)
+
+    commit()
+    commit(kc=a["contexts"][0].view(B._torch().uint8), vt=a["contexts"][0].view(B._torch().int16))
+    for bad in unfit_rows(a["rows"][0]):
+        for name in ("k", "v"):
+            with pytest.raises(ValueError):
+                commit(**{name: bad})
+    for bad in unfit_contexts(a["contexts"][0]):
+        for name in ("kc", "vt"):
+            with pytest.raises(ValueError):
+                commit(**{name: bad})
+
+
+def test_binding_attention_looks_at_shape_and_type(monkeypatch):
+    pool, plan, _, a = layered(monkeypatch)
+
+    def attend(**other):
+        x = {"k": a["rows"][0], "v": a["rows"][1], "kc": a["contexts"][0], "vt": a["contexts"][1], **other}
+        B.segmented_tree_attention(pool, plan, a["ints"], a["tree"], a["q"], x["k"], x["v"], x["kc"], x["vt"], a["q"].clone(), stream=0)
+
+    attend()
+    attend(kc=a["contexts"][0].view(B._torch().uint8), vt=a["contexts"][0].view(B._torch().int16))
+    for name in ("k", "v"):
+        for bad in unfit_rows(a["rows"][0]):
+            with pytest.raises(ValueError):
+                attend(**{name: bad})
+    for name in ("kc", "vt"):
+        for bad in unfit_contexts(a["contexts"][0]):
+            with pytest.raises(ValueError):
+                attend(**{name: bad})
+
+
 def test_oracle_trees_by_hand():
     assert tree.ways([-1, 0, 0, 1, -1, 4]) == [[0], [0, 1], [0, 2], [0, 1, 3], [4], [4, 5]]
     assert tree.ways([-1, -2, 1, 3, 5, 0]) == [[0], [], [], [], [], [0, 5]]
