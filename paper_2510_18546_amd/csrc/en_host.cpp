@@ -267,15 +267,25 @@ static int pool_ensure_device(en_pool *p)
         }
         rows(bound(shared), p->d.max_ctx);
     }
-    hipError_t e;
-    if ((e = hipMalloc((void **)&p->d_cos, n * sizeof(float))) != hipSuccess)
-        return hip_fail(e, "hipMalloc(rotary table)");
-    if ((e = hipMalloc((void **)&p->d_sin, n * sizeof(float))) != hipSuccess)
-        return hip_fail(e, "hipMalloc(rotary table)");
-    if ((e = hipMemcpy(p->d_cos, c.data(), n * sizeof(float), hipMemcpyHostToDevice)) != hipSuccess)
-        return hip_fail(e, "hipMemcpy(rotary table)");
-    if ((e = hipMemcpy(p->d_sin, s.data(), n * sizeof(float), hipMemcpyHostToDevice)) != hipSuccess)
-        return hip_fail(e, "hipMemcpy(rotary table)");
+    // (the pool has a table once it is whole: a call that could not set it up leaves the next one to try again)
+    float *tab[2] = {nullptr, nullptr};
+    const float *const from[2] = {c.data(), s.data()};
+    hipError_t e = hipSuccess;
+    const char *what = "hipMalloc(rotary table)";
+    for (int i = 0; i < 2 && e == hipSuccess; ++i)
+        e = hipMalloc((void **)&tab[i], n * sizeof(float));
+    for (int i = 0; i < 2 && e == hipSuccess; ++i) {
+        what = "hipMemcpy(rotary table)";
+        e = hipMemcpy(tab[i], from[i], n * sizeof(float), hipMemcpyHostToDevice);
+    }
+    if (e != hipSuccess) {
+        for (float *t : tab)
+            if (t)
+                (void)hipFree(t);
+        return hip_fail(e, what);
+    }
+    p->d_cos = tab[0];
+    p->d_sin = tab[1];
     // set-up is also where this device's address of the static scratch is looked up, so that
     // segmented_decode_step_static finds it ready (it asks again by itself if this failed)
     void *sp = nullptr;
