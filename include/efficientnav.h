@@ -379,6 +379,8 @@ int segmented_decode_step_static(en_pool *pool, en_plan *plan, int32_t q_first, 
  *   per step   segmented_tree_commit         (all layers in one launch)
  * Everything that changes from step to step is device memory, so that a loop
  * of steps needs no word from the host and can be captured into a HIP graph.
+ * (Under penalties that goes for the history too: the accepted tokens join it
+ * where the caller puts them there, see en_token_rules.)
  *
  * Trees. n_nodes <= EN_TREE_MAX_NODES drafted tokens per agent, the same number
  * for all, and
@@ -412,7 +414,7 @@ int segmented_decode_step_static(en_pool *pool, en_plan *plan, int32_t q_first, 
  *                            have scratch of their own (so has token_tree_accept)
  * Arrays of rows and contexts are 16-byte aligned. What absent nodes' rows
  * hold, or nodes outside a way, makes no difference, infinities and NaN
- * included.
+ * included. A visible key whose score is minus infinity has no weight.
  * Errors: INVALID_ARG (null, n_nodes < 1, alignment), UNSUPPORTED (n_nodes >
  *         EN_TREE_MAX_NODES, a plan whose values stay in the pool, 2^31 rows or
  *         contexts of 2^31 bytes per KV head), CAPACITY (ws_bytes), DEVICE.
@@ -435,7 +437,12 @@ int segmented_tree_attention(en_pool *pool, en_plan *plan, int32_t n_nodes, cons
  *   penalties_dev   : device float [B, 3]: repetition, frequency, presence
  *                     (1, 0, 0 changes nothing); read with the history
  *   history_dev     : device int32 [B, history_stride]; entries that are no
- *                     token (outside [0, vocab)) count nowhere. NULL: only ways
+ *                     token (outside [0, vocab)) count nowhere. NULL: only ways.
+ *                     No call here writes it: tokens of accepted nodes count in
+ *                     later steps once the caller has put them behind the
+ *                     agent's last entry and added n_accepted to history_len,
+ *                     in a kernel of its own behind token_tree_accept, which
+ *                     leaves path_dev for it
  *   history_len_dev : device int32 [B]; taken as 0 below it and as
  *                     history_stride beyond it
  *   bias_dev        : device float, row b at b * bias_agent_stride (0: one row

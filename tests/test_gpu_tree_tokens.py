@@ -516,3 +516,65 @@ def test_a_loop_of_drafted_steps(dtype, captured):
             used += len(p)
         assert np.array_equal(t.ddone.cpu().numpy(), t.done)
     assert used > steps and t.done[2] == n_new
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_loop_whose_history_grows(captured):
+    """The caller appends the accepted tokens to the history, on the device like everything else: choices of later steps are
+    those under all tokens so far. The logits stay what they are, so that without them a step's choices would be the ones
+    before again."""
+    import torch
+    from oracle import tree
+    from paper_2510_18546_amd import binding as B
+    agents, n, vocab, n_new, steps = 3, 6, 300, 60, 6
+    t = Tree(4, "bf16", [20, 3, 9], [0, 2, 5], n_new, [chain(n), comb(n), broken(n)], d=64, fill=0.0)
+    c = drawn(9, agents, n, vocab, "f32", 10, exact=True)
+    agree(c, t, np.random.default_rng(5), 1.0, much=40.0)
+    c["penalties"][:] = [2.0, 1.0, 4.0]
+    c["history_len"][:] = [4, 0, 10]
+    room = 10 + steps * n + 1                       # the last entry is where nothing is appended to
+    c["history"] = np.concatenate([c["history"], np.full((agents, room - 10), -1, np.int32)], 1)
+    history, length, penalties = (dev(c[k]) for k in ("history", "history_len", "penalties"))
+    rules = B.token_rules(penalties, history, length)
+    x, tokens = logits_on(c["logits"], "f32"), dev(c["tokens"])
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    choice, path = (torch.empty(agents, n, **i32) for _ in range(2))
+    count, token = (torch.empty(agents, **i32) for _ in range(2))
+    at = torch.arange(n, device="cuda:0")
+    ws = torch.empty(B.tree_accept_workspace_bytes(t.plan, n, vocab), dtype=torch.uint8, device="cuda:0")
+
+    def step():
+        B.token_tree_accept(t.plan, t.ddone, t.dparent, tokens, x, choice, path, count, token, t.ddone, ws, rules)
+        on = path >= 0
+        history.scatter_(1, torch.where(on, length[:, None] + at, room - 1), tokens.gather(1, path.clamp(min=0).long()))
+        length.add_(count)
+
+    graph = None
+    if captured:
+        kept = [z.clone() for z in (history, length, t.ddone)]
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for z, was in zip((history, length, t.ddone), kept):
+            z.copy_(was)
+    first = None
+    for _ in range(steps):
+        graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        want_x = tree.rules(c["logits"], t.parent, c["tokens"], c["penalties"], c["history"], c["history_len"])
+        want_choice = np.array([[tree.choose(r) for r in a] for a in want_x])
+        want = tree.accept(want_choice, t.done, n_new, t.parent, c["tokens"])
+        for b, (p, nxt) in enumerate(want):
+            assert list(path[b].cpu().numpy()[:len(p)]) == p and int(count[b]) == len(p) and int(token[b]) == nxt
+            h = int(c["history_len"][b])
+            c["history"][b, h:h + len(p)] = c["tokens"][b, p]
+            c["history_len"][b] += len(p)
+            t.done[b] += len(p)
+        assert np.array_equal(length.cpu().numpy(), c["history_len"])
+        assert np.array_equal(history.cpu().numpy()[:, :-1], c["history"][:, :-1])
+        first = want if first is None else first
+    assert want != first
