@@ -414,7 +414,8 @@ int segmented_decode_step_static(en_pool *pool, en_plan *plan, int32_t q_first, 
  *                            have scratch of their own (so has token_tree_accept)
  * Arrays of rows and contexts are 16-byte aligned. What absent nodes' rows
  * hold, or nodes outside a way, makes no difference, infinities and NaN
- * included. A visible key whose score is minus infinity has no weight.
+ * included. A visible key whose score is minus infinity has no weight,
+ * and a row none of whose keys has a weight is zero.
  * Errors: INVALID_ARG (null, n_nodes < 1, alignment), UNSUPPORTED (n_nodes >
  *         EN_TREE_MAX_NODES, a plan whose values stay in the pool, 2^31 rows or
  *         contexts of 2^31 bytes per KV head), CAPACITY (ws_bytes), DEVICE.

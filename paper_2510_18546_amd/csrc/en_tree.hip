@@ -639,7 +639,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW == 2 ? 1 : 2) __attribute__((
             for (int g = 0; g < 4; ++g)
                 op[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
     } else {
-        const float inv = row_valid ? 1.f / l : 0.f;
+        // (zero where no key has a weight, as a merge leaves it; by the bits: a sum of NaN stays one)
+        const float inv = row_valid && __float_as_uint(l) ? 1.f / l : 0.f;
         bf16_t *op = (bf16_t *)a.out + (((size_t)b * n + i_row) * a.Hq + hq) * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < NDB; ++d)

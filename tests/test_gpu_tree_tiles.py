@@ -7,8 +7,8 @@ e_j: its own rounding, at most 2^-8 and in the mean square 2^-8 / sqrt(3), and t
 of standard normal numbers (their D products over sqrt(D) are off by 2^-8 / sqrt(3) each in the mean square). The weights'
 sum is off by the same, so that the row is off by sum p_j e_j (v_j - out): in the mean square 2^-8 sqrt(2 / 3) times
 sqrt(sum p_j^2 |v_j - out|^2), which is computed beside the expected row; six times that is allowed. Drafted keys are
-rounded in the expected rows as they are held. A tile that is left out of n moves a row by 1 / sqrt(n) of its norm,
-six times as much as is allowed for the largest n here, 47. fp32: as in tree_cases.near."""
+rounded in the expected rows as they are held. A tile that is left out moves every row by more than that: by 2.4 to 16
+times as much, row by row, of the largest number here, 47, by 5 to 28 times as much of 13. fp32: as in tree_cases.near."""
 import numpy as np
 import pytest
 
@@ -149,6 +149,32 @@ def test_scores_that_jump_between_the_tiles_of_a_workgroup(dtype, d, r, n, agent
         units = agents * (2 if (r, n) == (7, 64) else 1)
         assert t.splits() == (1 if units >= 180 else 2)
     t.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d,r,n,agents", [("bf16", (64, 128)[(i + j) % 2], *shape, agents) for i, shape in enumerate(SHAPES)
+                                                for j, agents in enumerate((2, 260))] + [("f32", 64, 2, 13, 2), ("f32", 128, 4, 25, 260)])
+def test_rows_whose_keys_all_have_no_weight_are_zero(dtype, d, r, n, agents):
+    """Every score minus infinity, but those of one drafted key: rows that see it are its value's and those that do not are
+    zero, with one split and with several."""
+    import torch
+    first, second = d // 2 - 1, d - 1             # (the slowest pair, see test_scores_that_jump_between_the_tiles_of_a_workgroup)
+
+    def change(t):
+        for half in (first, second):
+            t.q[..., half] = bf16(np.abs(t.q[..., half]) + 0.5)
+        t.keys[..., first] = np.where(np.isnan(t.keys[..., first]), np.nan, -np.inf)
+        t.k[:, :, :2, :, first] = t.k[:, :, 3:, :, first] = -np.inf
+
+    t = Copies(n, dtype, agents, [130, 64], [1, 0], 80, forest(1, n) * 2, change, r=r, kv=1, d=d)
+    assert dtype == "f32" or (t.splits() == 1) == (agents == 260)
+    got = t.attend()
+    torch.cuda.synchronize()
+    got = got[:2].double().cpu().numpy()
+    for b in range(2):
+        for i, way in enumerate(tree.ways(t.parent[b])):
+            want = np.broadcast_to(t.v[0][b, 2, 0] if 2 in way else 0.0, got[b, i].shape)
+            assert np.array_equal(got[b, i], want), (b, i)
 
 
 @pytest.mark.gpu
