@@ -43,9 +43,9 @@ __device__ __forceinline__ void wave_lds_order()
 // ---------------------------------------------------------------------------
 // rules: a workgroup takes EN_RULES_CHUNK tokens of `a.nodes` of an agent's rows, a wave an equal share of the tokens of each
 // row: 16 a lane, in two runs of eight, or one run. Reading the logits once (and writing them once) is all that choices
-// without rules cost: 64 x 32 rows of 128000 tokens, bf16, 91 us, 5.8 TB/s; one agent's eight rows of 32000 3.8, which is a
+// without rules cost: 64 x 32 rows of 128000 tokens, bf16, 93 us, 5.6 TB/s; one agent's eight rows of 32000 3.8, which is a
 // launch and two trips to memory. Under penalties the tables' set-up comes first (7 us with 2 - 4 K tokens of history), then
-// the instructions a token: all rules on 16 x 13 rows of 50021 tokens 17.7 us, choices of 128000 under all rules 25.9.
+// the instructions a token: all rules on 16 x 13 rows of 50021 tokens 18.0 us, choices of 128000 under all rules 26.
 //
 // The tokens that penalties concern are few: they are counted into a table in LDS once for all rows of the workgroup, each
 // wave lists those of its share, and in a row only they are divided and subtracted from, in a copy of the share in
@@ -66,7 +66,7 @@ struct EnRulesLds {
 };
 
 // RULES: none, a bias or a mask, or penalties too. (One instance for all rules, which keeps 128 registers and half as many waves
-// where there are no penalties: choices of 64 x 32 rows of 128000 tokens under a bias and masks 161 us, now 110, of 16 x 13 18.5 /
+// where there are no penalties: choices of 64 x 32 rows of 128000 tokens under a bias and masks 161 us, so 110, of 16 x 13 18.5 /
 // 17.0; 16 x 13 rows of 50021 written out 13.1 / 12.8.)
 enum EnRulesKind { EN_NO_RULES, EN_FEW_RULES, EN_ALL_RULES };
 
@@ -298,7 +298,8 @@ void rules_kernel(EnRulesArgs a)
             // The largest of each run, of the wave, the first lane that has it in its first run or else in its second, and
             // which of the run's it is: of equals the lowest token. (NaN is no maximum. A maximum passes over a quiet NaN, but
             // of a signalling one, which logits may hold as they come from memory, the hardware makes NaN: canonical numbers
-            // are quiet.)
+            // are quiet. Without / with this, us: 64 x 32 rows of 128000 tokens 92 / 93, under a bias and masks 113 / 120, of 16 x
+            // 13 under a bias and masks 17.7 / 18.5.)
             float top_of[Q];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {

@@ -9,7 +9,7 @@
 // 16 K tokens x 4 nodes 766 us, 5.6 TB/s, as fast as a kernel that only reads), at 256 and more by feeding the matrix
 // instructions (64 nodes of 56 heads over 8 K tokens 27.8 us, 15.1 GFLOP: 5 us of start, then 1.8 us a tile of 64 keys), and a
 // short one by its start: arguments, the agent's header and counts, rows and angles are trips to memory one behind the other
-// (8 nodes over 1.5 K tokens 8.2 us). A workgroup takes up to 8 row blocks of 32 rows (a wave each) of a KV head and a split
+// (8 nodes over 1.5 K tokens 9.0 us). A workgroup takes up to 8 row blocks of 32 rows (a wave each) of a KV head and a split
 // of its keys; 64-key tiles of K and V^T go straight into LDS, NST of them in turn, and every wave reads all of them there.
 //
 // The tree's own keys are one more tile, the last split's first: the workgroup rotates them and lays them out in LDS as a
@@ -21,10 +21,12 @@
 // first keys a row sees and changes only where a score is 2^59 above it. The drafted keys, the probabilities and the output
 // are rounded to bf16 once each (what the products take); sums, references and what the splits leave for the merge are
 // float32. A query is the sum of two bf16 numbers (see cut_off) where up to four blocks of rows share a tile, and is rounded
-// once where eight do: the second product of its scores would be half as much again of what those steps
-// are bound by. (Outputs' error against 64 bits, 2-norm, 0.0021 / 0.0028, of which the output's own rounding is 0.0017. Two
-// parts / one, us: 8 nodes over 1.5 K tokens 8.7 / 8.2, 16 agents with 13 nodes over 2 K 32.4 / 30.6, 64 agents over 16 K
-// 772 / 771, 4 agents with 32 nodes over 4 K 26.1 / 24.1; 64 nodes of 56 heads over 8 K 35.0 in blocks of four / 28.0.)
+// once, as in the other bf16 attention calls, where eight do: the second product of its scores would be half as much again of
+// what those steps are bound by. (Outputs' error against 64 bits, 2-norm, 0.0021 - 0.0023 / 0.0029, of which the output's own
+// rounding is 0.0017. Two parts / one, us: 8 nodes over 1.5 K tokens 9.0 / 8.2, 16 agents with 13 nodes over 2 K 32.4 / 30.6,
+// 64 agents over 16 K 772 / 771, 4 agents with 32 nodes over 4 K 26.1 / 24.1. Eight blocks of 128 values in two parts spill, four
+// blocks by eight waves do not; these / eight blocks in one part, with the merge: 64 nodes of 56 heads over 8 K 39.7 / 34.0, 64
+// agents' 64 nodes over 2 K 257 / 179.)
 //
 // 16-byte chunks of a row lie in LDS exchanged by XOR with its number, so that 16 consecutive rows' reads of the same
 // chunk meet distinct banks; the loads bring them there by reading their source in that order.

@@ -145,9 +145,7 @@ def test_scores_that_jump_between_the_tiles_of_a_workgroup(dtype, d, r, n, agent
         t.k[..., c] = own
 
     t = Copies(n + d, dtype, agents, [9 * 64 - 5, 9 * 64 - 50, 8 * 64 + 3], [2, 0, 1], 80, forest(3, n), change, r=r, kv=1, d=d)
-    if dtype == "bf16":
-        units = agents * (2 if (r, n) == (7, 64) else 1)
-        assert t.splits() == (1 if units >= 180 else 2)
+    assert dtype == "f32" or t.splits() <= (1 if agents == 260 else 2)
     t.check()
 
 
