@@ -476,9 +476,14 @@ def _buffer(name: str, t, nbytes: int, dev: int) -> int:
     return t.data_ptr()
 
 
+def _other_numbers(x, dtype) -> bool:
+    """Numbers of another type than `dtype`, not bare bytes."""
+    return x is not dtype and (x.is_floating_point or x.is_complex)
+
+
 def _context(name: str, t, nbytes: int, dtype, dev: int) -> int:
     """Address of a context buffer, numbers of that type or bare bytes (as alloc_context makes them)."""
-    if t.dtype is not dtype and t.dtype.is_floating_point:
+    if _other_numbers(t.dtype, dtype):
         raise _unfit(name, t, f"a context of {dtype}")
     return _buffer(name, t, nbytes, dev)
 
@@ -496,7 +501,7 @@ def _layers_contexts(name: str, ts, nbytes: int, dtype, dev: int) -> array.array
     """Addresses of the layers' contexts (see _context)."""
     t_ = _torch().Tensor
     types = set(map(t_.dtype.__get__, ts))
-    if (min(map(t_.nbytes.__get__, ts)) < nbytes or types != {dtype} and any(x is not dtype and x.is_floating_point for x in types) or
+    if (min(map(t_.nbytes.__get__, ts)) < nbytes or types != {dtype} and any(_other_numbers(x, dtype) for x in types) or
             not all(map(t_.is_contiguous, ts)) or set(map(t_.get_device, ts)) != {dev}):
         raise ValueError(f"{name}: a contiguous context of at least {nbytes} bytes, {dtype} or bytes, on the current device is wanted "
                          "for every layer")

@@ -202,7 +202,7 @@ def unfit_rows(x):
 
 def unfit_contexts(x):
     import torch
-    return [x.float(), x.to(torch.float16), x.double(), x[:-1], torch.zeros(x.numel(), 2, dtype=x.dtype)[:, 0]]
+    return [x.float(), x.to(torch.float16), x.double(), x.to(torch.complex64), x[:-1], torch.zeros(x.numel(), 2, dtype=x.dtype)[:, 0]]
 
 
 def test_binding_commit_looks_at_shape_and_type_of_every_layer(monkeypatch):
